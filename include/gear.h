@@ -26,6 +26,10 @@
  *   gear_dense_forward /      events 2-3 and the second half of event 6 for a
  *   gear_dense_backward       linear Dense Part; gear_adam_dense and the adam
  *                             fields of gear_step_out: Section 4's optimiser.
+ *   gear_rms_norm, gear_q8_*  events 2-3 in 8 bits, for a Dense Part of normed
+ *                             layers; gear_rms_norm_backward: event 6 for them.
+ *   gear_clip_grads           the gradients' global norm and their clipping,
+ *                             ahead of the optimiser.
  *   gear_collect_expired      Section 1 / Section 3: cached inference results
  *                             older than the inference-expired time.
  *
@@ -76,7 +80,9 @@ enum {
 };
 
 /* element types of tables and of the head's matrix-product operands */
-enum { GEAR_F32 = 0, GEAR_BF16 = 1 };
+enum { GEAR_F32 = 0, GEAR_BF16 = 1,
+       GEAR_E4M3 = 2 };          /* 8-bit floating point with 4 exponent and 3 mantissa bits, largest value 448: outputs of
+                                    gear_rms_norm, operands of gear_q8_matmul.  Not a type of tables or heads */
 
 /* how gear_accumulate_dfv_grad combines rows that share an Image ID */
 enum {
@@ -382,6 +388,93 @@ int gear_dense_backward(gear_ctx* ctx, const float* raw, int32_t raw_dim, const 
  */
 int gear_adam_dense(float* param, const float* grad, float* m, float* v, int64_t n, int64_t t, const gear_adam* cfg,
                     void* stream);
+
+/*
+ * A Dense Part in 8 bits (Section 3, events 2 and 3, at scale: the features of every expired image go through it).  Rows are
+ * normed, put into e4m3 with one fp32 scale for every 128 columns, and multiplied by weights in e4m3 with one scale for every
+ * 128 x 128 of them.  A layer is gear_rms_norm, then gear_q8_matmul; the last product's fp32 rows are what gear_refresh_dfv takes.
+ * These calls need no ctx.  General to them:
+ *   - a row k stands at ptr + k * ld (ld in elements, at least the number of columns); any alignment of an element's own size and
+ *     any ld will do unless said otherwise (16-byte aligned rows are read and written faster);
+ *   - d_n (device, optional): only rows k < min(n, *d_n) are computed, *d_n read when the kernel runs; the others stay as they were;
+ *   - status (device, two words, zero before the first call; optional unless said otherwise): GEAR_DEV_* bits are added to
+ *     status[0]; status[1] is non-zero once a bounded wait has given up (GEAR_DEV_TIMEOUT), and until the caller clears it.
+ *     Calls on streams that may overlap each have a status of their own;
+ *   - inputs and outputs do not overlap, except where said.
+ *
+ * The 8-bit form of a row h of `cols` values, block by block of GEAR_Q8_BLOCK columns (the last one may be shorter):
+ *     scale = max(max_j |h_j|, 2^-100) / 448,    q_j = h_j / scale rounded to e4m3 (nearest even).
+ * A block that holds a NaN has a NaN for its scale and in all its values; one that holds an infinity and no NaN has an infinite scale,
+ * NaN in the infinite places and zeros elsewhere.
+ */
+enum { GEAR_Q8_BLOCK = 128 };
+
+/*
+ * Root-mean-square norm, with what surrounds it.  For k < n:
+ *     y = x[ids ? ids[k] : k] (+ res[k]),  rounded to the input type;   res_out[k] = y
+ *     h = y / sqrt(mean_j y_j^2 + eps) * weight;                        out[k] = h in out_dtype
+ * x, res, res_out: dtype GEAR_F32 or GEAR_BF16.  ids (device, optional): rows of x by ID in [0, vocab); an ID outside counts as a row of zeros and
+ * raises GEAR_DEV_BAD_ID.  res, res_out: optional, each without the other too; res_out may be res, or x where ids is NULL.
+ * weight: fp32 [cols], optional (ones).  out_dtype GEAR_F32, GEAR_BF16 (scale NULL) or GEAR_E4M3 with scale fp32 [n][ceil(cols / 128)].
+ * Sums are fp32; with a GEAR_E4M3 output h is not rounded to any other type in between.
+ */
+int gear_rms_norm(const void* x, int64_t ldx, int32_t dtype, const int32_t* ids, int64_t vocab, const void* res, int64_t ld_res,
+                  void* res_out, int64_t ld_res_out, const float* weight, int64_t n, const int64_t* d_n, int32_t cols, float eps,
+                  void* out, int64_t ld_out, int32_t out_dtype, float* scale, int32_t* status, void* stream);
+
+/*
+ * Its gradients.  x: the normed rows (the y of gear_rms_norm); dout: the gradient of h; with r = 1 / sqrt(mean_j x_j^2 + eps) and
+ * g = dout * weight, for k < n (and k < *d_n):
+ *     dx[k] = r g - x r^3 (sum_j g_j x_j) / cols (+ dres[k]);      dweight_j = sum_k dout[k]_j x[k]_j r[k]   (written, not added to)
+ * x, dout, dres (optional: the gradient that reaches y past the norm), dx: dtype.  ids / vocab as above (for x alone; then dx and dres belong to row k).
+ * dx or dweight may be NULL; dx may be dout or dres.  8-bit outputs count as unrounded.  workspace: fp32
+ * [GEAR_NORM_WORKSPACE_ROWS][cols], 16-byte aligned, when dweight is given.  Results do not depend on timing.
+ */
+enum { GEAR_NORM_WORKSPACE_ROWS = 592 };
+int gear_rms_norm_backward(const void* x, int64_t ldx, int32_t dtype, const int32_t* ids, int64_t vocab, const float* weight,
+                           const void* dout, int64_t ld_dout, const void* dres, int64_t ld_dres, int64_t n, const int64_t* d_n,
+                           int32_t cols, float eps, void* dx, int64_t ld_dx, float* dweight, float* workspace, int32_t* status,
+                           void* stream);
+
+/* Rows in their 8-bit form without a norm: q[k], scale[k] of x[k] (the operand of a product back through a layer). */
+int gear_q8_rows(const void* x, int64_t ldx, int32_t dtype, int64_t n, const int64_t* d_n, int32_t cols, void* q, int64_t ldq,
+                 float* scale, void* stream);
+
+/*
+ * Weights W [K][N] (fp32, row k at W + k * ldw) as gear_q8_matmul reads them: q [N][ldq >= K] e4m3, scale [ceil(N / 128)][ceil(K / 128)], one for
+ * every 128 x 128 block by the same formula; and the same values transposed, for the gradient of the layer's input: q_t [K][ldq_t >= N],
+ * scale_t [ceil(K / 128)][ceil(N / 128)].  Either pair may be NULL.
+ */
+int gear_q8_weights(const float* W, int64_t ldw, int32_t K, int32_t N, void* q, int64_t ldq, float* scale, void* q_t, int64_t ldq_t,
+                    float* scale_t, void* stream);
+
+/*
+ * out[m][j] = sum_kb a_scale[m][kb] b_scale[j / 128][kb] (sum over k of block kb of a[m][k] b[j][k]),  m < n, j < N, blocks of 128 along K.
+ * a [n][lda], b [N][ldb] e4m3, 16-byte aligned, lda and ldb multiples of 16 (what lies in a row behind K is not used);
+ * a_scale [n][ceil(K / 128)], b_scale [ceil(N / 128)][ceil(K / 128)].  out_dtype GEAR_F32 or GEAR_BF16.  Products are exact, sums fp32.
+ * Scales and products outside fp32's range become infinities or zeros as fp32 has it.  status: required.
+ */
+int gear_q8_matmul(const void* a, int64_t lda, const float* a_scale, const void* b, int64_t ldb, const float* b_scale, int64_t n,
+                   const int64_t* d_n, int32_t N, int32_t K, void* out, int64_t ld_out, int32_t out_dtype, int32_t* status, void* stream);
+
+/*
+ * The global norm of gradients, and their clipping (between a backward pass and the optimiser):
+ *     norm[0] = sqrt(sum over all tensors of sum_i g_i^2)                                (sums in 64 bits)
+ *     gear_clip_grads: norm[1] = c = min(1, max_norm / (norm[0] + 1e-6)),  out_i = c g_i  rounded to the tensor's type
+ * grads: host array of `count` tensors; grad: device, n values of dtype GEAR_F32 or GEAR_BF16, any alignment of a value's own size; out: the tensor's grad
+ * itself (which is left untouched where c = 1) or memory that overlaps no tensor of the call; not read by gear_grad_norm.
+ * A tensor may be empty, the list too (norm 0, c = 1).  norm: device fp32 [2].  A norm that is not finite is not hidden: an infinity among the
+ * gradients gives c = 0 and a NaN in its place, a NaN gives NaN everywhere.  workspace: device, GEAR_CLIP_WORKSPACE_BYTES, 8-byte aligned,
+ * one for every stream; nothing in it carries over from one call to the next.  Results do not depend on timing.
+ */
+enum { GEAR_CLIP_WORKSPACE_BYTES = 32768 };
+typedef struct {
+    const void* grad; void* out;
+    int64_t n;
+    int32_t dtype;
+} gear_grad;
+int gear_grad_norm(const gear_grad* grads, int32_t count, float* norm, void* workspace, void* stream);
+int gear_clip_grads(const gear_grad* grads, int32_t count, float max_norm, float* norm, void* workspace, void* stream);
 
 /*
  * Synchronises the stream last used; returns the device status word (GEAR_DEV_* bits, then cleared) and

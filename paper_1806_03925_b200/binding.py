@@ -17,7 +17,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libgear.so")
 
 GEAR_OK, GEAR_ERR_ARG, GEAR_ERR_CAPACITY, GEAR_ERR_BAD_ID, GEAR_ERR_CUDA, GEAR_ERR_STATE = 0, -1, -2, -3, -4, -5
-GEAR_F32, GEAR_BF16 = 0, 1
+GEAR_F32, GEAR_BF16, GEAR_E4M3 = 0, 1, 2
 GEAR_ACC_SORT, GEAR_ACC_ATOMIC = 0, 1
 GEAR_DEV_BAD_ID, GEAR_DEV_READY_OVERFLOW, GEAR_DEV_OUT_CAPACITY, GEAR_DEV_BAD_CSR = 1, 2, 4, 8
 GEAR_TAG_USER, GEAR_TAG_URL, GEAR_TAG_DFV, GEAR_TAG_TS, GEAR_TAG_GRAD = 1, 2, 3, 4, 5
@@ -28,9 +28,13 @@ EXPORTS = ("gear_workspace_bytes", "gear_init_tables", "gear_forward_backward", 
            "gear_last_error", "gear_profile_enable", "gear_profile_read", "gear_launch_count",
            "gear_collect_expired_static", "gear_refresh_dfv", "gear_accumulate_collect", "gear_dense_forward",
            "gear_dense_backward", "gear_adam_dense", "gear_fetch_rows", "gear_apply_emb_grad", "gear_profile_timeline", "gear_step",
-           "gear_shard_stage_words", "gear_shard_host_words", "gear_shard_step")
+           "gear_shard_stage_words", "gear_shard_host_words", "gear_shard_step", "gear_rms_norm", "gear_rms_norm_backward",
+           "gear_q8_rows", "gear_q8_weights", "gear_q8_matmul", "gear_grad_norm", "gear_clip_grads")
 GEAR_STATIC_EXPIRY_MAX_VOCAB = 16777216
 GEAR_MAX_LOCAL_RANKS = 8
+GEAR_Q8_BLOCK = 128
+GEAR_NORM_WORKSPACE_ROWS = 592
+GEAR_CLIP_WORKSPACE_BYTES = 32768
 
 
 class GearError(RuntimeError):
@@ -84,6 +88,10 @@ class gear_shard_plan(C.Structure):
 class gear_host_batch(C.Structure):
     _fields_ = [("B", C.c_int32), ("nnz", C.c_int64), ("user_id", C.c_void_p), ("url_id", C.c_void_p), ("img_off", C.c_void_p),
                 ("img_id", C.c_void_p), ("label", C.c_void_p)]
+
+
+class gear_grad(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32)]
 
 
 _lib = None
@@ -151,6 +159,21 @@ def load() -> C.CDLL:
     L.gear_launch_count.argtypes = [vp, C.POINTER(i64)]
     L.gear_collect_expired_static.restype = C.c_int
     L.gear_collect_expired_static.argtypes = [vp, i64, i64, i64, C.c_int, vp, i64, vp, C.POINTER(i64), vp]
+    f32 = C.c_float
+    L.gear_rms_norm.restype = C.c_int
+    L.gear_rms_norm.argtypes = [vp, i64, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, i32, f32, vp, i64, i32, vp, vp, vp]
+    L.gear_rms_norm_backward.restype = C.c_int
+    L.gear_rms_norm_backward.argtypes = [vp, i64, i32, vp, i64, vp, vp, i64, vp, i64, i64, vp, i32, f32, vp, i64, vp, vp, vp, vp]
+    L.gear_q8_rows.restype = C.c_int
+    L.gear_q8_rows.argtypes = [vp, i64, i32, i64, vp, i32, vp, i64, vp, vp]
+    L.gear_q8_weights.restype = C.c_int
+    L.gear_q8_weights.argtypes = [vp, i64, i32, i32, vp, i64, vp, vp, i64, vp, vp]
+    L.gear_q8_matmul.restype = C.c_int
+    L.gear_q8_matmul.argtypes = [vp, i64, vp, vp, i64, vp, i64, vp, i32, i32, vp, i64, i32, vp, vp]
+    L.gear_grad_norm.restype = C.c_int
+    L.gear_grad_norm.argtypes = [vp, i32, vp, vp, vp]
+    L.gear_clip_grads.restype = C.c_int
+    L.gear_clip_grads.argtypes = [vp, i32, f32, vp, vp, vp]
     L.gear_last_error.restype = C.c_char_p
     L.gear_last_error.argtypes = []
     _lib = L
@@ -382,6 +405,229 @@ def gear_adam_dense(param, grad, m, v, t: int, cfg: gear_adam, stream=None):
     rc = (_lib or load()).gear_adam_dense(_p(param), _p(grad), _p(m), _p(v), n, t, cfg, _raw_stream(stream))
     if rc != GEAR_OK:
         _check(rc, "gear_adam_dense")
+
+
+# ---------------------------------------------------------------------------
+# a Dense Part in 8 bits, clipping: calls without a ctx.  Rows may be views (any distance between rows, the values of a row one
+# behind the other); all tensors of a call are on the current device.
+# ---------------------------------------------------------------------------
+_FLOATS = {torch.float32: GEAR_F32, torch.bfloat16: GEAR_BF16}
+_OUTS = {torch.float32: GEAR_F32, torch.bfloat16: GEAR_BF16, torch.float8_e4m3fn: GEAR_E4M3, torch.uint8: GEAR_E4M3}
+
+
+def _refuse(what: str):
+    raise TypeError("libgear: " + what)
+
+
+def _rows(t: torch.Tensor, dtypes, dev: int, n: Optional[int] = None, cols: Optional[int] = None):
+    """(pointer, distance between rows, type) of a 2-D tensor of rows, with at least n of them and exactly cols columns."""
+    if t.get_device() != dev:
+        _refuse("takes device memory of the current device; got a %s tensor" % t.device)
+    code = dtypes.get(t.dtype)
+    if code is None:
+        _refuse("does not take %s here" % t.dtype)
+    if t.dim() != 2 or (cols is not None and t.shape[1] != cols) or (n is not None and t.shape[0] < n):
+        _refuse("rows of shape %s; needed: %s x %s" % (tuple(t.shape), "any" if n is None else n, "any" if cols is None else cols))
+    ld, one = t.stride()
+    if one != 1 and t.shape[1] > 1:
+        _refuse("takes rows whose values lie one behind the other")
+    return t.data_ptr(), ld if t.shape[0] > 1 else max(ld, t.shape[1]), code
+
+
+def _vec(t: Optional[torch.Tensor], dtype, dev: int, n: Optional[int] = None):
+    """Pointer of a contiguous tensor of at least n values (None -> NULL)."""
+    if t is None:
+        return None
+    if t.get_device() != dev or t.dtype != dtype or not t.is_contiguous() or (n is not None and t.numel() < n):
+        _refuse("needs a contiguous %s tensor of the current device%s; got %s %s on %s" %
+                (dtype, "" if n is None else " with at least %d values" % n, tuple(t.shape), t.dtype, t.device))
+    return t.data_ptr()
+
+
+def _stream_here(stream: Optional[torch.cuda.Stream], dev: int) -> int:
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(dev)
+    if stream.device_index != dev:
+        _refuse("the stream is not one of the current device")
+    return stream.cuda_stream
+
+
+def _row_count(n: Optional[int], t: torch.Tensor) -> int:
+    have = t.shape[0]
+    if n is None:
+        return have
+    if n < 0 or n > have:
+        _refuse("n = %d outside [0, %d]" % (n, have))
+    return n
+
+
+def _blocks(cols: int) -> int:
+    return (cols + GEAR_Q8_BLOCK - 1) // GEAR_Q8_BLOCK
+
+
+def gear_rms_norm(x, weight, out, scale=None, eps: float = 1e-6, res=None, res_out=None, ids=None, n: Optional[int] = None,
+                  d_n=None, status=None, stream=None):
+    """out[k] = RMS norm of x[k] (of x[ids[k]]) (+ res[k]) times weight, for k < n (default: all rows of out); out fp32, bf16 or, with
+    scale, e4m3.  res_out[k] gets the sum."""
+    dev = torch._C._cuda_getDevice()
+    n = _row_count(n, out)
+    xp, ldx, code = _rows(x, _FLOATS, dev, None if ids is not None else n)
+    cols = x.shape[1]
+    same = {x.dtype: code}
+    rp, ldr, _ = (None, 0, 0) if res is None else _rows(res, same, dev, n, cols)
+    sp, lds, _ = (None, 0, 0) if res_out is None else _rows(res_out, same, dev, n, cols)
+    op, ldo, out_code = _rows(out, _OUTS, dev, n, cols)
+    rc = (_lib or load()).gear_rms_norm(
+        xp, ldx, code, _vec(ids, torch.int32, dev, n), x.shape[0], rp, ldr, sp, lds, _vec(weight, torch.float32, dev, cols), n,
+        _vec(d_n, torch.int64, dev, 1), cols, eps, op, ldo, out_code, _vec(scale, torch.float32, dev, n * _blocks(cols)),
+        _vec(status, torch.int32, dev, 2), _stream_here(stream, dev))
+    if rc != GEAR_OK:
+        _check(rc, "gear_rms_norm")
+
+
+def gear_rms_norm_backward(x, weight, dout, dx, dweight, workspace, eps: float = 1e-6, dres=None, ids=None, n: Optional[int] = None,
+                           d_n=None, status=None, stream=None):
+    """Gradients of gear_rms_norm from x (the sum it normed) and dout: dx[k] (+ dres[k]) and dweight, either of which may be None;
+    workspace: fp32 [GEAR_NORM_WORKSPACE_ROWS][cols], with dweight."""
+    dev = torch._C._cuda_getDevice()
+    n = _row_count(n, dout)
+    xp, ldx, code = _rows(x, _FLOATS, dev, None if ids is not None else n)
+    cols = x.shape[1]
+    same = {x.dtype: code}
+    gp, ldg, _ = _rows(dout, same, dev, n, cols)
+    rp, ldr, _ = (None, 0, 0) if dres is None else _rows(dres, same, dev, n, cols)
+    dp, ldd, _ = (None, 0, 0) if dx is None else _rows(dx, same, dev, n, cols)
+    if dweight is not None and workspace is None:
+        _refuse("dweight needs a workspace")
+    rc = (_lib or load()).gear_rms_norm_backward(
+        xp, ldx, code, _vec(ids, torch.int32, dev, n), x.shape[0], _vec(weight, torch.float32, dev, cols), gp, ldg, rp, ldr, n,
+        _vec(d_n, torch.int64, dev, 1), cols, eps, dp, ldd, _vec(dweight, torch.float32, dev, cols),
+        None if dweight is None else _vec(workspace, torch.float32, dev, GEAR_NORM_WORKSPACE_ROWS * cols),
+        _vec(status, torch.int32, dev, 2), _stream_here(stream, dev))
+    if rc != GEAR_OK:
+        _check(rc, "gear_rms_norm_backward")
+
+
+_E4M3 = {torch.float8_e4m3fn: GEAR_E4M3, torch.uint8: GEAR_E4M3}
+
+
+def gear_q8_rows(x, q, scale, n: Optional[int] = None, d_n=None, stream=None):
+    """q[k], scale[k] = x[k] in e4m3, one scale for every 128 columns."""
+    dev = torch._C._cuda_getDevice()
+    n = _row_count(n, q)
+    xp, ldx, code = _rows(x, _FLOATS, dev, n)
+    cols = x.shape[1]
+    qp, ldq, _ = _rows(q, _E4M3, dev, n, cols)
+    if scale is None:
+        _refuse("scale is needed")
+    rc = (_lib or load()).gear_q8_rows(xp, ldx, code, n, _vec(d_n, torch.int64, dev, 1), cols, qp, ldq,
+                                       _vec(scale, torch.float32, dev, n * _blocks(cols)), _stream_here(stream, dev))
+    if rc != GEAR_OK:
+        _check(rc, "gear_q8_rows")
+
+
+def gear_q8_weights(W, q=None, scale=None, q_t=None, scale_t=None, stream=None):
+    """W [K][N] fp32 in e4m3 as gear_q8_matmul reads it: q [N][K] and its scales, and / or q_t [K][N] and its scales."""
+    dev = torch._C._cuda_getDevice()
+    wp, ldw, _ = _rows(W, {torch.float32: GEAR_F32}, dev)
+    K, N = W.shape
+    qp, ldq, _ = (None, 0, 0) if q is None else _rows(q, _E4M3, dev, N, K)
+    tp, ldt, _ = (None, 0, 0) if q_t is None else _rows(q_t, _E4M3, dev, K, N)
+    blocks = _blocks(K) * _blocks(N)
+    rc = (_lib or load()).gear_q8_weights(wp, ldw, K, N, qp, ldq, _vec(scale, torch.float32, dev, blocks), tp, ldt,
+                                          _vec(scale_t, torch.float32, dev, blocks), _stream_here(stream, dev))
+    if rc != GEAR_OK:
+        _check(rc, "gear_q8_weights")
+
+
+def gear_q8_matmul(a, a_scale, b, b_scale, out, status, n: Optional[int] = None, d_n=None, stream=None):
+    """out[m] = a[m] . b^T with the scales of both, m < n (default: all rows of out); a [n][K], b [N][K] e4m3, rows at multiples of
+    16 bytes; out fp32 or bf16 [n][N]; status: int32 [2], zero before the first call."""
+    dev = torch._C._cuda_getDevice()
+    n = _row_count(n, out)
+    ap, lda, _ = _rows(a, _E4M3, dev, n)
+    K = a.shape[1]
+    bp, ldb, _ = _rows(b, _E4M3, dev, None, K)
+    N = b.shape[0]
+    op, ldo, code = _rows(out, _FLOATS, dev, n, N)
+    if n == 1:                                       # (a single row's distance to the next one does not matter)
+        lda = (lda + 15) & ~15
+    if N == 1:
+        ldb = (ldb + 15) & ~15
+    if a_scale is None or b_scale is None:
+        _refuse("both scales are needed")
+    rc = (_lib or load()).gear_q8_matmul(ap, lda, _vec(a_scale, torch.float32, dev, n * _blocks(K)), bp, ldb,
+                                         _vec(b_scale, torch.float32, dev, _blocks(N) * _blocks(K)), n, _vec(d_n, torch.int64, dev, 1), N, K,
+                                         op, ldo, code, _vec(status, torch.int32, dev, 2), _stream_here(stream, dev))
+    if rc != GEAR_OK:
+        _check(rc, "gear_q8_matmul")
+
+
+class GradList:
+    """The C form of a list of gradients (make_grads); keeps the tensors alive."""
+    __slots__ = ("items", "count", "device", "tensors")
+
+
+def make_grads(grads: Sequence[torch.Tensor], outs: Optional[Sequence[torch.Tensor]] = None) -> GradList:
+    """The list gear_grad_norm and gear_clip_grads take, made once by a program whose gradients stay where they are.  outs: where the
+    clipped gradients go (default: in place)."""
+    where = grads if outs is None else outs
+    if len(where) != len(grads):
+        _refuse("as many outs as grads")
+    l = GradList()
+    l.device = torch._C._cuda_getDevice()
+    l.items, l.count, l.tensors = (gear_grad * max(1, len(grads)))(), len(grads), (list(grads), list(where))
+    written = set()
+    for i, (g, o) in enumerate(zip(grads, where)):
+        code, at, to = _FLOATS.get(g.dtype), g.data_ptr(), o.data_ptr()
+        if code is None or o.dtype != g.dtype or o.numel() != g.numel():
+            _refuse("gradients are fp32 or bf16, each out like its gradient")
+        if g.get_device() != l.device or o.get_device() != l.device:
+            _refuse("takes device memory of the current device")
+        if not (g.is_contiguous() and o.is_contiguous()):
+            _refuse("takes contiguous gradients")
+        if g.numel() and to in written:
+            _refuse("a gradient is written twice")
+        written.add(to)
+        l.items[i] = (at, to, g.numel(), code)
+    return l
+
+
+def _grads(grads, outs=None) -> GradList:
+    l = grads if isinstance(grads, GradList) else make_grads(grads, outs)
+    if l is grads and outs is not None:
+        _refuse("a list made with make_grads has its outs already")
+    if l.device != torch._C._cuda_getDevice():
+        _refuse("the gradients are not on the current device")
+    return l
+
+
+def gear_grad_norm(grads, norm, workspace, stream=None):
+    """norm[0] = the 2-norm of all gradients together (a list of tensors, or what make_grads returned)."""
+    dev = torch._C._cuda_getDevice()
+    if not isinstance(grads, GradList):
+        grads = make_grads(grads, grads)
+    l = _grads(grads)
+    rc = (_lib or load()).gear_grad_norm(l.items, l.count, _vec(norm, torch.float32, dev, 1), _clip_workspace(workspace, dev), _stream_here(stream, dev))
+    if rc != GEAR_OK:
+        _check(rc, "gear_grad_norm")
+
+
+def gear_clip_grads(grads, max_norm: float, norm, workspace, outs=None, stream=None):
+    """out_i = c g_i with c = min(1, max_norm / (norm + 1e-6)); norm (fp32 [2]) gets the norm and c.  grads: a list of tensors (clipped in
+    place, or into outs), or what make_grads returned."""
+    dev = torch._C._cuda_getDevice()
+    l = _grads(grads, outs)
+    rc = (_lib or load()).gear_clip_grads(l.items, l.count, max_norm, _vec(norm, torch.float32, dev, 2), _clip_workspace(workspace, dev),
+                                          _stream_here(stream, dev))
+    if rc != GEAR_OK:
+        _check(rc, "gear_clip_grads")
+
+
+def _clip_workspace(t: torch.Tensor, dev: int):
+    if t.get_device() != dev or not t.is_contiguous() or t.numel() * t.element_size() < GEAR_CLIP_WORKSPACE_BYTES:
+        _refuse("the workspace: GEAR_CLIP_WORKSPACE_BYTES of contiguous memory of the current device")
+    return t.data_ptr()
 
 
 def gear_status(ctx, raise_on_error: bool = False):

@@ -935,6 +935,113 @@ int gear_adam_dense(float* param, const float* grad, float* m, float* v, int64_t
     return e == cudaSuccess ? GEAR_OK : cuda_fail(e, "adam_dense");
 }
 
+// ---------------------------------------------------------------- a Dense Part in 8 bits, clipping (no ctx)
+static int dtype_size(int32_t dtype) { return dtype == GEAR_E4M3 ? 1 : dtype == GEAR_BF16 ? 2 : 4; }
+static bool aligned_to(const void* p, int32_t dtype) { return reinterpret_cast<uintptr_t>(p) % (uintptr_t)dtype_size(dtype) == 0; }
+
+// what gear_rms_norm and its gradients share
+static int check_norm(const NormArgs& a, int32_t dtype) {
+    if (dtype != GEAR_F32 && dtype != GEAR_BF16) return arg_fail("dtype: GEAR_F32 or GEAR_BF16");
+    if (a.n < 0 || a.n > INT32_MAX) return arg_fail("n outside [0, 2^31 - 1]");
+    if (a.cols < 1) return arg_fail("cols >= 1");
+    if (!(a.eps >= 0.f)) return arg_fail("eps >= 0");
+    if (a.ids && (a.vocab < 1 || a.vocab > INT32_MAX)) return arg_fail("vocab outside [1, 2^31 - 1]");
+    if (a.n > 0 && (!a.x || a.ldx < a.cols || !aligned_to(a.x, dtype))) return arg_fail("x: NULL, misaligned or ldx < cols");
+    if (a.weight && !aligned_to(a.weight, GEAR_F32)) return arg_fail("weight: misaligned");
+    return GEAR_OK;
+}
+static bool bad_rows(const void* p, int64_t ld, int32_t cols, int32_t dtype) { return ld < cols || !aligned_to(p, dtype); }
+static int32_t q8_blocks(int32_t cols) { return (int32_t)ceil_div(cols, GEAR_Q8_BLOCK); }
+
+static int finish(cudaError_t e, const char* where) { return e == cudaSuccess ? GEAR_OK : cuda_fail(e, where); }
+
+int gear_rms_norm(const void* x, int64_t ldx, int32_t dtype, const int32_t* ids, int64_t vocab, const void* res, int64_t ld_res,
+                  void* res_out, int64_t ld_res_out, const float* weight, int64_t n, const int64_t* d_n, int32_t cols, float eps,
+                  void* out, int64_t ld_out, int32_t out_dtype, float* scale, int32_t* status, void* stream) {
+    NormArgs a{};
+    a.x = x; a.ldx = ldx; a.ids = ids; a.vocab = vocab; a.res = res; a.ld_res = ld_res; a.res_out = res_out; a.ld_res_out = ld_res_out;
+    a.weight = weight; a.n = n; a.d_n = d_n; a.cols = cols; a.eps = eps; a.normed = 1;
+    a.out = out; a.ld_out = ld_out; a.out_dtype = out_dtype; a.scale = scale; a.blocks = q8_blocks(cols); a.status = status;
+    if (int rc = check_norm(a, dtype)) return rc;
+    if (out_dtype != GEAR_F32 && out_dtype != GEAR_BF16 && out_dtype != GEAR_E4M3) return arg_fail("out_dtype");
+    if ((out_dtype == GEAR_E4M3) != (scale != nullptr)) return arg_fail("scale: for GEAR_E4M3 outputs, and only for them");
+    if (n == 0) return GEAR_OK;
+    if (!out || bad_rows(out, ld_out, cols, out_dtype)) return arg_fail("out: NULL, misaligned or ld_out < cols");
+    if ((res && bad_rows(res, ld_res, cols, dtype)) || (res_out && bad_rows(res_out, ld_res_out, cols, dtype)))
+        return arg_fail("res, res_out: misaligned or ld < cols");
+    if (scale && !aligned_to(scale, GEAR_F32)) return arg_fail("scale: misaligned");
+    return finish(no_throw([&] { return launch_rms_norm(a, dtype, static_cast<cudaStream_t>(stream)); }), "rms_norm");
+}
+
+int gear_q8_rows(const void* x, int64_t ldx, int32_t dtype, int64_t n, const int64_t* d_n, int32_t cols, void* q, int64_t ldq, float* scale,
+                 void* stream) {
+    NormArgs a{};
+    a.x = x; a.ldx = ldx; a.n = n; a.d_n = d_n; a.cols = cols;
+    a.out = q; a.ld_out = ldq; a.out_dtype = GEAR_E4M3; a.scale = scale; a.blocks = q8_blocks(cols);
+    if (int rc = check_norm(a, dtype)) return rc;
+    if (n == 0) return GEAR_OK;
+    if (!q || !scale || ldq < cols || !aligned_to(scale, GEAR_F32)) return arg_fail("q, scale: NULL, misaligned or ldq < cols");
+    return finish(no_throw([&] { return launch_rms_norm(a, dtype, static_cast<cudaStream_t>(stream)); }), "q8_rows");
+}
+
+int gear_rms_norm_backward(const void* x, int64_t ldx, int32_t dtype, const int32_t* ids, int64_t vocab, const float* weight,
+                           const void* dout, int64_t ld_dout, const void* dres, int64_t ld_dres, int64_t n, const int64_t* d_n,
+                           int32_t cols, float eps, void* dx, int64_t ld_dx, float* dweight, float* workspace, int32_t* status, void* stream) {
+    NormArgs a{};
+    a.x = x; a.ldx = ldx; a.ids = ids; a.vocab = vocab; a.weight = weight; a.n = n; a.d_n = d_n; a.cols = cols; a.eps = eps;
+    a.dout = dout; a.ld_dout = ld_dout; a.dres = dres; a.ld_dres = ld_dres; a.dx = dx; a.ld_dx = ld_dx;
+    a.dweight = dweight; a.parts = dweight ? workspace : nullptr; a.status = status;
+    if (int rc = check_norm(a, dtype)) return rc;
+    if (!dx && !dweight) return arg_fail("dx and dweight are both NULL");
+    if (dweight && (!aligned_to(dweight, GEAR_F32) || !workspace || !aligned16(workspace))) return arg_fail("dweight needs a workspace, 16-byte aligned");
+    if (n > 0) {
+        if (!dout || bad_rows(dout, ld_dout, cols, dtype)) return arg_fail("dout: NULL, misaligned or ld < cols");
+        if ((dx && bad_rows(dx, ld_dx, cols, dtype)) || (dres && bad_rows(dres, ld_dres, cols, dtype))) return arg_fail("dx, dres: misaligned or ld < cols");
+    }
+    return finish(no_throw([&] { return launch_rms_norm_backward(a, dtype, static_cast<cudaStream_t>(stream)); }), "rms_norm_backward");
+}
+
+int gear_q8_weights(const float* W, int64_t ldw, int32_t K, int32_t N, void* q, int64_t ldq, float* scale, void* q_t, int64_t ldq_t,
+                    float* scale_t, void* stream) {
+    if (K < 1 || N < 1 || !W || ldw < N || !aligned_to(W, GEAR_F32)) return arg_fail("K, N >= 1; W: NULL, misaligned or ldw < N");
+    if ((!q && !q_t) || (q && (!scale || ldq < K)) || (q_t && (!scale_t || ldq_t < N))) return arg_fail("q, q_t: one of them, each with its scales, rows long enough");
+    return finish(no_throw([&] {
+        return launch_q8_weights(W, ldw, K, N, static_cast<uint8_t*>(q), ldq, scale, static_cast<uint8_t*>(q_t), ldq_t, scale_t, static_cast<cudaStream_t>(stream));
+    }), "q8_weights");
+}
+
+int gear_q8_matmul(const void* a, int64_t lda, const float* a_scale, const void* b, int64_t ldb, const float* b_scale, int64_t n,
+                   const int64_t* d_n, int32_t N, int32_t K, void* out, int64_t ld_out, int32_t out_dtype, int32_t* status, void* stream) {
+    if (n < 0 || n > INT32_MAX - 128 || N < 1 || K < 1) return arg_fail("n in [0, 2^31 - 129], N, K >= 1");
+    if (out_dtype != GEAR_F32 && out_dtype != GEAR_BF16) return arg_fail("out_dtype: GEAR_F32 or GEAR_BF16");
+    if (!status) return arg_fail("status: required");
+    if (n == 0) return GEAR_OK;
+    if (!a || !b || !a_scale || !b_scale || !out) return arg_fail("NULL pointer");
+    if (!aligned16(a) || !aligned16(b) || (lda & 15) || (ldb & 15) || lda < K || ldb < K) return arg_fail("a, b: 16-byte aligned, rows a multiple of 16 bytes apart, at least K");
+    if (!aligned_to(a_scale, GEAR_F32) || !aligned_to(b_scale, GEAR_F32) || bad_rows(out, ld_out, N, out_dtype)) return arg_fail("scales or out: misaligned, or ld_out < N");
+    const Q8Args q{static_cast<const uint8_t*>(a), lda, a_scale, static_cast<const uint8_t*>(b), ldb, b_scale, n, d_n, N, K, out, ld_out, out_dtype, status};
+    return finish(no_throw([&] { return launch_q8_product(q, static_cast<cudaStream_t>(stream)); }), "q8_matmul");
+}
+
+static int clip_call(const gear_grad* grads, int32_t count, bool clip, float max_norm, float* norm, void* workspace, void* stream) {
+    if (count < 0 || (count > 0 && !grads) || !norm || !workspace || reinterpret_cast<uintptr_t>(workspace) % 8 || !aligned_to(norm, GEAR_F32))
+        return arg_fail("grads, norm, workspace: NULL or misaligned");
+    if (clip && !(max_norm >= 0.f)) return arg_fail("max_norm >= 0");
+    for (int32_t i = 0; i < count; ++i) {
+        const gear_grad& g = grads[i];
+        if (g.dtype != GEAR_F32 && g.dtype != GEAR_BF16) return arg_fail("a gradient's dtype: GEAR_F32 or GEAR_BF16");
+        if (g.n < 0 || g.n > (1ll << 48)) return arg_fail("a gradient's n");
+        if (g.n > 0 && (!g.grad || !aligned_to(g.grad, g.dtype) || (clip && (!g.out || !aligned_to(g.out, g.dtype))))) return arg_fail("a gradient's grad or out: NULL or misaligned");
+    }
+    return finish(no_throw([&] { return launch_clip(grads, count, clip, max_norm, norm, workspace, static_cast<cudaStream_t>(stream)); }), clip ? "clip_grads" : "grad_norm");
+}
+int gear_grad_norm(const gear_grad* grads, int32_t count, float* norm, void* workspace, void* stream) {
+    return clip_call(grads, count, false, 0.f, norm, workspace, stream);
+}
+int gear_clip_grads(const gear_grad* grads, int32_t count, float max_norm, float* norm, void* workspace, void* stream) {
+    return clip_call(grads, count, true, max_norm, norm, workspace, stream);
+}
+
 int gear_status(gear_ctx* ctx, int32_t* device_status, int64_t* pending_ready) {
     if (!ctx || !ctx->impl.alive) return GEAR_ERR_STATE;
     gear_ctx_impl& c = ctx->impl;

@@ -602,21 +602,24 @@ static EncodeTiledFn encode_fn() {
     return fn;
 }
 
-bool TmaCache::get(CUtensorMap* out, const TmaSpec& k) {
-    for (int i = 0; i < used_; ++i)
-        if (key_[i] == k) { *out = map_[i]; return true; }
+bool encode_map(CUtensorMap* out, const TmaSpec& k) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
-    const cuuint64_t esz = k.f32 ? 4 : 2;
+    const cuuint64_t esz = k.f32 == 1 ? 4 : k.f32 == 2 ? 1 : 2;
     cuuint64_t dims[3] = {(cuuint64_t)k.cols, (cuuint64_t)k.rows, (cuuint64_t)k.planes};
     cuuint64_t strides[2] = {(cuuint64_t)k.ld * esz, (cuuint64_t)k.plane_stride * esz};
     cuuint32_t box[3] = {(cuuint32_t)k.box_cols, (cuuint32_t)k.box_rows, (cuuint32_t)k.planes};
     cuuint32_t estr[3] = {1, 1, 1};
-    if (fn(out, k.f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, k.planes > 1 ? 3 : 2,
-           const_cast<void*>(k.ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-           k.swizzle == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-        return false;
+    return fn(out, k.f32 == 1 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : k.f32 == 2 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
+              k.planes > 1 ? 3 : 2, const_cast<void*>(k.ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              k.swizzle == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool TmaCache::get(CUtensorMap* out, const TmaSpec& k) {
+    for (int i = 0; i < used_; ++i)
+        if (key_[i] == k) { *out = map_[i]; return true; }
+    if (!encode_map(out, k)) return false;
     const int i = used_ < N ? used_++ : (next_ = (next_ + 1) % N);
     key_[i] = k; map_[i] = *out;
     return true;

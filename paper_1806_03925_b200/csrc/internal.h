@@ -228,6 +228,44 @@ cudaError_t launch_emb_adam_rows(const gear_ctx_impl& c, const EmbAdamTable& t0,
 cudaError_t launch_emb_adam(const gear_ctx_impl& c, int buf, int32_t B, const float* dX, int ldx, const gear_adam& cfg,
                             int64_t t, float* user_m, float* user_v, float* url_m, float* url_v, cudaStream_t st);
 
+// clip.cu: global norm of a list of gradients and, with clip, the clipped ones
+cudaError_t launch_clip(const gear_grad* g, int32_t count, bool clip, float max_norm, float* norm, void* workspace, cudaStream_t st);
+
+// norm.cu: what the arguments of gear_rms_norm, gear_q8_rows and gear_rms_norm_backward come to
+struct NormArgs {
+    const void* x; int64_t ldx;
+    const int32_t* ids; int64_t vocab;
+    const void* res; int64_t ld_res;
+    void* res_out; int64_t ld_res_out;
+    const float* weight;
+    int64_t n; const int64_t* d_n;
+    int cols; float eps;
+    int normed;                                  // 0: the 8-bit form alone
+    void* out; int64_t ld_out; int out_dtype;
+    float* scale; int blocks;                    // blocks of a row
+    int32_t* status;
+    // the gradients (backward)
+    const void* dout; int64_t ld_dout;
+    const void* dres; int64_t ld_dres;
+    void* dx; int64_t ld_dx;
+    float* dweight; float* parts;
+};
+cudaError_t launch_rms_norm(const NormArgs& a, int dtype, cudaStream_t st);
+cudaError_t launch_rms_norm_backward(const NormArgs& a, int dtype, cudaStream_t st);
+cudaError_t launch_q8_weights(const float* W, int64_t ldw, int K, int N, uint8_t* q, int64_t ldq, float* scale, uint8_t* qt, int64_t ldqt,
+                              float* scale_t, cudaStream_t st);
+
+// q8_product.cu
+struct Q8Args {
+    const uint8_t* a; int64_t lda; const float* a_scale;
+    const uint8_t* b; int64_t ldb; const float* b_scale;
+    int64_t n; const int64_t* d_n;
+    int N, K;
+    void* out; int64_t ld_out; int out_dtype;
+    int32_t* status;
+};
+cudaError_t launch_q8_product(const Q8Args& q, cudaStream_t st);
+
 // shard.cu: row fetch for a table shard's owner; event 5's gradient rows in materialised form
 cudaError_t launch_fetch_rows(const gear_ctx_impl& c, int which, const int32_t* ids, int64_t n, void* out, cudaStream_t st);
 cudaError_t launch_dfv_grad_rows(const gear_ctx_impl& c, const float* dX, const int32_t* row_view, const float* inv_n,

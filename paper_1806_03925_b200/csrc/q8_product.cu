@@ -1,0 +1,344 @@
+// Products of e4m3 rows with e4m3 weights, an fp32 scale for every 128 columns of a row and every 128 x 128 weights
+// (gear_q8_matmul), on the 5th-generation tensor cores:
+//
+//     out[m][j] = sum_kb a_scale[m][kb] b_scale[j / 128][kb] (sum over k of block kb of a[m][k] b[j][k])
+//
+// The scales change with every block of 128 along K, so a block's products are a tile of their own: tcgen05.mma leaves them in one
+// of a ring of accumulators in tensor memory, and the epilogue warps add them, times the two scales, to sums in registers while the
+// tensor cores fill the next accumulator.  A warp's columns lie in one block of weights and a lane holds one row, so a lane has one
+// factor per block of K; two columns are multiplied and added per instruction (fma.rn.f32x2).
+//
+// One persistent kernel, a CTA per SM: warp 0 streams the operands in by TMA (boxes of 128 bytes along K, which are one block),
+// warp 1 issues the products (M 128, N BN, K 32: four per block), warps 2 to 9 add up and store.  Two warps share a quarter of the
+// tensor-memory lanes and split the columns.  Every wait is bounded: on a timeout the kernel says so in the status words, leaves
+// its loops, frees its tensor memory and returns.  No cluster launch and no multicast.
+#include "internal.h"
+#include "q8.cuh"
+#include "tc_ptx.cuh"
+
+namespace gear {
+
+constexpr int QP_EW = 8;                                     // epilogue warps
+constexpr int QP_THREADS = 64 + 32 * QP_EW;
+constexpr int QP_OUT_BLOCK = 32 * 128;                       // a warp's results on their way out: 32 rows of 128 bytes
+
+template <int BN> struct QpCfg {
+    static constexpr int A_BYTES = TC_BM * Q8_BLOCK, B_BYTES = BN * Q8_BLOCK, STAGE_BYTES = A_BYTES + B_BYTES;
+    static constexpr int STAGES = BN == 256 ? 4 : 6;
+    static constexpr int ACCS = BN == 256 ? 2 : 4;           // accumulators: all of the tensor memory, or half of it
+    static constexpr int TMEM_COLS = BN * ACCS;
+    static constexpr int SMEM = STAGES * STAGE_BYTES + QP_EW * QP_OUT_BLOCK + 1024 /*alignment slack*/ + 256 /*barriers*/;
+    static_assert(SMEM <= 227 * 1024 && SMEM > 116 * 1024, "one CTA per SM: two would both ask for tensor memory");
+};
+
+struct QpArgs {
+    const float* a_scale; const float* b_scale;
+    int64_t n; const int64_t* d_n;
+    int N, K, n_tiles;
+    void* out; int64_t ld_out; int vec;                      // vec: rows of out may be written 16 bytes at a time
+    int32_t* status;
+};
+
+__device__ __forceinline__ uint64_t pair64(uint32_t lo, uint32_t hi) { return (uint64_t)lo | (uint64_t)hi << 32; }
+__device__ __forceinline__ void fma_pair(uint64_t& acc, uint64_t v, uint64_t s) { asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc) : "l"(v), "l"(s)); }
+
+// A warp's 32 rows x 128 bytes from shared memory (16-byte pieces XOR-swizzled by the row) to the output: eight lanes per row.
+template <typename T>
+__device__ __forceinline__ void qp_store_block(uint32_t block, T* out, int64_t ld, int64_t m0, int64_t live, int n0, int N, bool vec, int lane) {
+    constexpr int PER = 16 / (int)sizeof(T);
+    const int piece = lane & 7, col = n0 + piece * PER;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int row = i * 4 + (lane >> 3);
+        uint4 v;
+        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                     : "r"(block + (uint32_t)row * 128u + (((uint32_t)(piece ^ (row & 7))) << 4)) : "memory");
+        if (m0 + row >= live || col >= N) continue;
+        T* dst = out + (m0 + row) * ld + col;
+        if (vec && col + PER <= N) *reinterpret_cast<uint4*>(dst) = v;
+        else {
+            const T* e = reinterpret_cast<const T*>(&v);
+#pragma unroll
+            for (int j = 0; j < PER; ++j) if (col + j < N) dst[j] = e[j];
+        }
+    }
+}
+
+template <int BN, typename T>
+__global__ void __launch_bounds__(QP_THREADS, 1)
+q8_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const QpArgs g) {
+    using Cfg = QpCfg<BN>;
+    constexpr int STAGES = Cfg::STAGES, ACCS = Cfg::ACCS, COLS = BN / 2;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw);
+    const uint32_t tiles = (raw + 1023u) & ~1023u;
+    const uint32_t out_blocks = tiles + STAGES * Cfg::STAGE_BYTES;
+    const uint32_t bars = out_blocks + QP_EW * QP_OUT_BLOCK;
+    auto full_bar = [&](int s) { return bars + 8u * s; };
+    auto empty_bar = [&](int s) { return bars + 8u * (STAGES + s); };
+    auto acc_full = [&](int a) { return bars + 8u * (2 * STAGES + a); };
+    auto acc_empty = [&](int a) { return bars + 8u * (2 * STAGES + ACCS + a); };
+    const uint32_t tmem_word = bars + 8u * (2 * STAGES + 2 * ACCS);
+    volatile uint32_t* tmem_word_ptr = reinterpret_cast<volatile uint32_t*>(smem_raw + (tmem_word - raw));
+    int32_t* err = g.status + 1;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
+        for (int a = 0; a < ACCS; ++a) { mbar_init(acc_full(a), 1); mbar_init(acc_empty(a), 32 * QP_EW); }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("prefetch.tensormap [%0];" :: "l"(&map_a) : "memory");
+        asm volatile("prefetch.tensormap [%0];" :: "l"(&map_b) : "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                     :: "r"(tmem_word), "r"((uint32_t)Cfg::TMEM_COLS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_word_ptr;
+    wait_for_predecessor();
+
+    int64_t live = g.n;
+    if (g.d_n) { const int64_t d = *g.d_n; live = d < live ? (d < 0 ? 0 : d) : live; }
+    const int kbs = (g.K + Q8_BLOCK - 1) / Q8_BLOCK;
+    const int64_t total = (live + TC_BM - 1) / TC_BM * g.n_tiles;
+
+    if (warp == 0) {
+        // ---------------- TMA producer
+        if (lane == 0) {
+            uint32_t it = 0;
+            bool ok = true;
+            for (int64_t t = blockIdx.x; t < total && ok; t += gridDim.x) {
+                const int nt = (int)(t % g.n_tiles), mt = (int)(t / g.n_tiles);      // the column tiles of a row tile side by side
+                for (int kb = 0; kb < kbs; ++kb, ++it) {
+                    const int s = it % STAGES;
+                    if (!(ok = mbar_wait(empty_bar(s), ((it / STAGES) & 1u) ^ 1u, err, 1))) break;
+                    const uint32_t a_dst = tiles + s * Cfg::STAGE_BYTES, b_dst = a_dst + Cfg::A_BYTES;
+                    mbar_expect_tx(full_bar(s), Cfg::STAGE_BYTES);
+                    tma_load_2d(a_dst, &map_a, full_bar(s), kb * Q8_BLOCK, mt * TC_BM);
+                    tma_load_2d(b_dst, &map_b, full_bar(s), kb * Q8_BLOCK, nt * BN);
+                }
+            }
+            if (*reinterpret_cast<volatile int32_t*>(err) != 0) {
+                // leaving early: let the copies already issued land before the CTA gives its shared memory back
+                const uint32_t first = it > (uint32_t)STAGES ? it - STAGES : 0u;
+                for (uint32_t j = first; j < it; ++j)
+                    for (uint32_t spin = 0; spin < (1u << 16) && !mbar_try(full_bar(j % STAGES), (j / STAGES) & 1u); ++spin)
+                        __nanosleep(64);
+            }
+        }
+    } else if (warp == 1) {
+        // ---------------- MMA issuer
+        if (lane == 0) {
+            constexpr uint32_t idesc = instr_desc_e4m3(BN);
+            uint32_t it = 0;
+            bool ok = true;
+            for (int64_t t = blockIdx.x; t < total && ok; t += gridDim.x) {
+                for (int kb = 0; kb < kbs; ++kb, ++it) {
+                    const int s = it % STAGES, a = it % ACCS;
+                    if (!(ok = mbar_wait(acc_empty(a), ((it / ACCS) & 1u) ^ 1u, err, 2))) break;
+                    if (!(ok = mbar_wait(full_bar(s), (it / STAGES) & 1u, err, 3))) break;
+                    tc_fence_after();
+                    const uint32_t a_src = tiles + s * Cfg::STAGE_BYTES, b_src = a_src + Cfg::A_BYTES;
+#pragma unroll
+                    for (int k = 0; k < Q8_BLOCK / 32; ++k)
+                        tc_mma_f8(tmem_base + (uint32_t)(a * BN), smem_desc(a_src + k * 32, 16, 1024), smem_desc(b_src + k * 32, 16, 1024), idesc, k > 0 ? 1u : 0u);
+                    tc_commit(empty_bar(s));
+                    tc_commit(acc_full(a));
+                }
+            }
+        }
+    } else {
+        // ---------------- epilogue warps
+        const int quarter = warp & 3, part = (warp - 2) >> 2;
+        const uint32_t block = out_blocks + (uint32_t)(warp - 2) * QP_OUT_BLOCK;
+        const uint32_t t_lane = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(part * COLS);
+        uint32_t it = 0;
+        bool ok = true;
+        for (int64_t t = blockIdx.x; t < total && ok; t += gridDim.x) {
+            const int nt = (int)(t % g.n_tiles);
+            const int64_t m0 = t / g.n_tiles * TC_BM + quarter * 32, m = m0 + lane;
+            const int n0 = nt * BN + part * COLS;
+            const float* sa = m < live ? g.a_scale + m * kbs : nullptr;
+            const float* sb = n0 < g.N ? g.b_scale + (int64_t)(n0 / Q8_BLOCK) * kbs : nullptr;
+            uint64_t acc[COLS / 2];
+#pragma unroll
+            for (int i = 0; i < COLS / 2; ++i) acc[i] = 0ull;
+            float s_next = sa && sb ? __ldg(sa) * __ldg(sb) : 0.f;
+            for (int kb = 0; kb < kbs; ++kb, ++it) {
+                const uint32_t s32 = __float_as_uint(s_next);
+                if (kb + 1 < kbs && sa && sb) s_next = __ldg(sa + kb + 1) * __ldg(sb + kb + 1);      // on its way during the wait
+                const int a = it % ACCS;
+                if (!(ok = mbar_wait(acc_full(a), (it / ACCS) & 1u, err, 4))) break;
+                __syncwarp();
+                tc_fence_after();
+                const uint64_t s2 = pair64(s32, s32);
+                uint32_t r[2][16];
+                tc_ld16(t_lane + (uint32_t)(a * BN), r[0]);
+#pragma unroll
+                for (int c = 0; c < COLS / 16; ++c) {
+                    tc_wait_ld(r[c & 1]);
+                    if (c + 1 < COLS / 16) tc_ld16(t_lane + (uint32_t)(a * BN + (c + 1) * 16), r[(c + 1) & 1]);
+                    else { tc_fence_before(); mbar_arrive_relaxed(acc_empty(a)); }      // all of it has been read
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) fma_pair(acc[c * 8 + i], pair64(r[c & 1][2 * i], r[c & 1][2 * i + 1]), s2);
+                }
+            }
+            if (!ok) break;
+            // a lane's row leaves in pieces of 128 bytes through the warp's block
+            T* out = static_cast<T*>(g.out);
+            constexpr int PIECE = 128 / (int)sizeof(T);
+            static_assert(COLS >= PIECE || sizeof(T) == 2, "a piece is whole or half full");
+#pragma unroll
+            for (int c = 0; c < (COLS + PIECE - 1) / PIECE; ++c) {
+                if (n0 + c * PIECE >= g.N) break;             // (uniform over the warp)
+                __syncwarp();                                 // the block's previous contents have been read
+                const uint32_t row = block + (uint32_t)lane * 128u;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    uint32_t w[4] = {0u, 0u, 0u, 0u};
+                    if (sizeof(T) == 4) {
+                        const int i = c * (PIECE / 2) + 2 * j;
+                        w[0] = (uint32_t)acc[i]; w[1] = (uint32_t)(acc[i] >> 32); w[2] = (uint32_t)acc[i + 1]; w[3] = (uint32_t)(acc[i + 1] >> 32);
+                    } else {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const int i = c * (PIECE / 2) + 4 * j + q;
+                            if (i >= COLS / 2) continue;      // (32 columns: half a piece)
+                            const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float((uint32_t)acc[i]), __uint_as_float((uint32_t)(acc[i] >> 32)));
+                            w[q] = *reinterpret_cast<const uint32_t*>(&h);
+                        }
+                    }
+                    sts_u4(row + ((((uint32_t)j) ^ (uint32_t)(lane & 7)) << 4), make_uint4(w[0], w[1], w[2], w[3]));
+                }
+                __syncwarp();
+                const int edge = min(g.N, n0 + COLS);         // (of half a piece: the other half is another warp's)
+                qp_store_block<T>(block, out, g.ld_out, m0, live, n0 + c * PIECE, edge, g.vec != 0, lane);
+            }
+        }
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem_base), "r"((uint32_t)Cfg::TMEM_COLS) : "memory");
+        if (lane == 0 && *reinterpret_cast<volatile int32_t*>(err) != 0) atomicOr(g.status, GEAR_DEV_TIMEOUT);
+    }
+}
+
+// ---------------------------------------------------------------- few rows
+// Up to QF_ROWS rows at a time: the weights are read once and what there is to compute is little, so a warp has a column of the
+// output and reads its weights 16 bytes a lane (eight lanes per block of 128).  e4m3 values and their products are exact in fp32.
+constexpr int QF_ROWS = 8;
+
+__device__ __forceinline__ void e4m3_to_f32(const uint4& v, float (&f)[16]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[i >> 1] >> (16 * (i & 1))), __NV_E4M3);
+        const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&h));
+        f[2 * i] = p.x; f[2 * i + 1] = p.y;
+    }
+}
+// 16 bytes of a row from byte k on, with zeros from K on
+__device__ __forceinline__ uint4 load_bytes(const uint8_t* row, int k, int K) {
+    uint4 v = __ldg(reinterpret_cast<const uint4*>(row + k));
+    if (k + 16 > K) {
+        uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int left = K - k - 4 * i;                   // bytes of this word that count
+            if (left < 4) w[i] = left <= 0 ? 0u : w[i] & ((1u << (8 * left)) - 1u);
+        }
+    }
+    return v;
+}
+
+template <int R, typename T>
+__global__ void __launch_bounds__(128)
+q8_few_rows_kernel(const Q8Args g) {
+    wait_for_predecessor();
+    int64_t live = g.n;
+    if (g.d_n) { const int64_t d = *g.d_n; live = d < live ? (d < 0 ? 0 : d) : live; }
+    const int lane = threadIdx.x & 31, j = blockIdx.x * 4 + (threadIdx.x >> 5);
+    const int64_t m0 = (int64_t)blockIdx.y * R;
+    if (j >= g.N || m0 >= live) return;
+    const int rows = (int)min((int64_t)R, live - m0), kbs = (g.K + Q8_BLOCK - 1) / Q8_BLOCK;
+    const uint8_t* b = g.b + (int64_t)j * g.ldb;
+    const float* sb = g.b_scale + (int64_t)(j / Q8_BLOCK) * kbs;
+    float acc[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) acc[r] = 0.f;
+    for (int k = lane * 16; k < g.K; k += 512) {
+        const int kb = k / Q8_BLOCK;
+        const uint4 bv = load_bytes(b, k, g.K);
+        const float s = __ldg(sb + kb);
+        uint4 av[R];
+        float sa[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int64_t m = m0 + (r < rows ? r : 0);
+            av[r] = load_bytes(g.a + m * g.lda, k, g.K);
+            sa[r] = __ldg(g.a_scale + m * kbs + kb);
+        }
+        float w[16];
+        e4m3_to_f32(bv, w);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            float x[16], p = 0.f;
+            e4m3_to_f32(av[r], x);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) p = fmaf(x[i], w[i], p);
+            acc[r] = fmaf(p, sa[r] * s, acc[r]);
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const float v = warp_sum(acc[r]);
+        if (lane == 0 && r < rows) static_cast<T*>(g.out)[(m0 + r) * g.ld_out + j] = (T)v;
+    }
+}
+
+// ---------------------------------------------------------------- host side
+template <int BN, typename T> static cudaError_t qp_go(const Q8Args& q, cudaStream_t st) {
+    using Cfg = QpCfg<BN>;
+    constexpr auto kernel = q8_product_kernel<BN, T>;
+    if (const cudaError_t e = allow_smem<kernel>(Cfg::SMEM)) return e;
+    CUtensorMap ma, mb;
+    if (!encode_map(&ma, TmaSpec{q.a, q.n, q.K, q.lda, 0, 1, TC_BM, Q8_BLOCK, 2, 128}) || !encode_map(&mb, TmaSpec{q.b, q.N, q.K, q.ldb, 0, 1, BN, Q8_BLOCK, 2, 128}))
+        return cudaErrorInvalidValue;
+    QpArgs g = {};
+    g.a_scale = q.a_scale; g.b_scale = q.b_scale; g.n = q.n; g.d_n = q.d_n; g.N = q.N; g.K = q.K;
+    g.n_tiles = (int)ceil_div(q.N, BN);
+    g.out = q.out; g.ld_out = q.ld_out; g.status = q.status;
+    g.vec = (reinterpret_cast<uintptr_t>(q.out) & 15u) == 0 && (q.ld_out * (int64_t)sizeof(T)) % 16 == 0;
+    const int64_t tiles = ceil_div(q.n, TC_BM) * g.n_tiles;
+    const int grid = tiles < sm_count() ? (int)tiles : sm_count();
+    return launch_dependent(kernel, dim3(grid), dim3(QP_THREADS), (size_t)Cfg::SMEM, st, ma, mb, g);
+}
+template <int R, typename T> static cudaError_t qf_go(const Q8Args& q, cudaStream_t st) {
+    return launch_dependent(q8_few_rows_kernel<R, T>, dim3((unsigned)ceil_div(q.N, 4), (unsigned)ceil_div(q.n, R)), dim3(128), 0, st, q);
+}
+
+template <typename T> static cudaError_t qp_launch(const Q8Args& q, cudaStream_t st) {
+    if (q.n == 1) return qf_go<1, T>(q, st);
+    if (q.n <= 2) return qf_go<2, T>(q, st);
+    if (q.n <= 4) return qf_go<4, T>(q, st);
+    if (q.n <= QF_ROWS) return qf_go<QF_ROWS, T>(q, st);
+    // the widest tiles that leave no SM without one
+    const int64_t m_tiles = ceil_div(q.n, TC_BM);
+    if (q.N <= 64 || m_tiles * ceil_div(q.N, 64) <= sm_count()) return qp_go<64, T>(q, st);
+    if (q.N <= 128 || m_tiles * ceil_div(q.N, 128) <= sm_count()) return qp_go<128, T>(q, st);
+    return qp_go<256, T>(q, st);
+}
+
+cudaError_t launch_q8_product(const Q8Args& q, cudaStream_t st) {
+    if (q.n <= 0) return cudaSuccess;
+    return q.out_dtype == GEAR_BF16 ? qp_launch<__nv_bfloat16>(q, st) : qp_launch<float>(q, st);
+}
+
+}  // namespace gear

@@ -94,6 +94,13 @@ __device__ __forceinline__ void tc_mma(uint32_t d_tmem, uint64_t a_desc, uint64_
                  "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
                  :: "r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
 }
+// the same for operands of 8-bit floating point (K 32)
+__device__ __forceinline__ void tc_mma_f8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\t"
+                 "setp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+                 :: "r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
 __device__ __forceinline__ void tc_ld32(uint32_t taddr, uint32_t (&r)[32]) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
                  "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
@@ -152,6 +159,11 @@ __host__ __device__ constexpr uint32_t instr_desc(int bn, bool mn_major) {
            ((uint32_t)(bn >> 3) << 17) | ((uint32_t)(TC_BM >> 4) << 24);
 }
 
+// e4m3 x e4m3 -> fp32 (both format fields 0), both K-major
+__host__ __device__ constexpr uint32_t instr_desc_e4m3(int bn) {
+    return (1u << 4) | ((uint32_t)(bn >> 3) << 17) | ((uint32_t)(TC_BM >> 4) << 24);
+}
+
 // One warp of the grid: the batch's loss from the partial losses the kernel before this one left.
 __device__ __forceinline__ void sum_loss(const LossSum& s, int lane) {
     if (s.loss == nullptr) return;
@@ -168,13 +180,15 @@ struct TmaSpec {
     const void* ptr;
     int64_t rows, cols, ld, plane_stride;      // ld and plane_stride in elements
     int planes, box_rows, box_cols;
-    int f32;                                   // fp32 elements, else bf16
+    int f32;                                   // 1: fp32 elements, 0: bf16, 2: bytes
     int swizzle;                               // 128 or 64 bytes (= the bytes of a box row)
     bool operator==(const TmaSpec& o) const {
         return ptr == o.ptr && rows == o.rows && cols == o.cols && ld == o.ld && plane_stride == o.plane_stride &&
                planes == o.planes && box_rows == o.box_rows && box_cols == o.box_cols && f32 == o.f32 && swizzle == o.swizzle;
     }
 };
+
+bool encode_map(CUtensorMap* out, const TmaSpec& k);
 
 // A step encodes the same two dozen maps every time (operands and outputs live at fixed places in the workspace): every ctx
 // keeps its most recent encodings, which saves the driver calls.  A map depends on its spec alone.  (One table shared by all
