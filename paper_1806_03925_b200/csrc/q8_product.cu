@@ -9,7 +9,7 @@
 // factor per block of K; two columns are multiplied and added per instruction (fma.rn.f32x2).
 //
 // One persistent kernel, a CTA per SM: warp 0 streams the operands in by TMA (boxes of 128 bytes along K, which are one block),
-// warp 1 issues the products (M 128, N BN, K 32: four per block), warps 2 to 9 add up and store.  Two warps share a quarter of the
+// warps 1 and 2 issue the products (M 128, N BN, K 32: four per block), warps 4 to 11 add up and store.  Two warps share a quarter of the
 // tensor-memory lanes and split the columns.  Every wait is bounded: on a timeout the kernel says so in the status words, leaves
 // its loops, frees its tensor memory and returns.  No cluster launch and no multicast.
 #include "internal.h"
@@ -19,15 +19,16 @@
 namespace gear {
 
 constexpr int QP_EW = 8;                                     // epilogue warps
-constexpr int QP_THREADS = 64 + 32 * QP_EW;
-constexpr int QP_OUT_BLOCK = 32 * 128;                       // a warp's results on their way out: 32 rows of 128 bytes
+constexpr int QP_THREADS = 128 + 32 * QP_EW;                 // a warpgroup of producer, issuers and one that idles; the epilogue's two
+constexpr int QP_OUT_BLOCK = 32 * 128;                       // a warp's results on their way out: 32 rows of 128 bytes, two of these a warp
 
 template <int BN> struct QpCfg {
     static constexpr int A_BYTES = TC_BM * Q8_BLOCK, B_BYTES = BN * Q8_BLOCK, STAGE_BYTES = A_BYTES + B_BYTES;
-    static constexpr int STAGES = BN == 256 ? 4 : 6;
+    static constexpr int STAGES = BN == 256 ? 3 : BN == 128 ? 5 : 6;
     static constexpr int ACCS = BN == 256 ? 2 : 4;           // accumulators: all of the tensor memory, or half of it
     static constexpr int TMEM_COLS = BN * ACCS;
-    static constexpr int SMEM = STAGES * STAGE_BYTES + QP_EW * QP_OUT_BLOCK + 1024 /*alignment slack*/ + 256 /*barriers*/;
+    static constexpr bool SPLIT = BN == 256;                 // registers are handed from the first warpgroup to the others
+    static constexpr int SMEM = STAGES * STAGE_BYTES + QP_EW * 2 * QP_OUT_BLOCK + 1024 /*alignment slack*/ + 256 /*barriers*/;
     static_assert(SMEM <= 227 * 1024 && SMEM > 116 * 1024, "one CTA per SM: two would both ask for tensor memory");
 };
 
@@ -35,45 +36,81 @@ struct QpArgs {
     const float* a_scale; const float* b_scale;
     int64_t n; const int64_t* d_n;
     int N, K, n_tiles;
-    void* out; int64_t ld_out; int vec;                      // vec: rows of out may be written 16 bytes at a time
+    void* out; int64_t ld_out; int vec;                      // vec: rows of out start on 16-byte boundaries: map_out is set
     int32_t* status;
 };
+
+// Registers of a CTA with 128 columns a warp: launched with 168 a thread (384 x 168 = 64512), the epilogue's two warpgroups take 232,
+// the first one keeps 40 (256 x 232 + 128 x 40 = 64512).
+constexpr int QP_REGS_FEW = 40, QP_REGS_MANY = 232;
+
+__device__ __forceinline__ void qp_ld(uint32_t addr, uint32_t (&r)[32]) { tc_ld32(addr, r); }
+__device__ __forceinline__ void qp_ld(uint32_t addr, uint32_t (&r)[16]) { tc_ld16(addr, r); }
+
+// One lane waits for its warp.
+__device__ __forceinline__ bool qp_warp_wait(uint32_t bar, uint32_t parity, int32_t* err, int lane) {
+    bool ok = true;
+    if (lane == 0) ok = mbar_wait(bar, parity, err, 4);
+    return __all_sync(0xffffffffu, ok);
+}
 
 __device__ __forceinline__ uint64_t pair64(uint32_t lo, uint32_t hi) { return (uint64_t)lo | (uint64_t)hi << 32; }
 __device__ __forceinline__ void fma_pair(uint64_t& acc, uint64_t v, uint64_t s) { asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc) : "l"(v), "l"(s)); }
 
 // A warp's 32 rows x 128 bytes from shared memory (16-byte pieces XOR-swizzled by the row) to the output: eight lanes per row.
+// out: the block's first row and column; rows, cols: how much of it there is to write.
 template <typename T>
-__device__ __forceinline__ void qp_store_block(uint32_t block, T* out, int64_t ld, int64_t m0, int64_t live, int n0, int N, bool vec, int lane) {
+__device__ __forceinline__ void qp_store_block(uint32_t block, T* out, int64_t ld, int rows, int cols, bool vec, int lane) {
     constexpr int PER = 16 / (int)sizeof(T);
-    const int piece = lane & 7, col = n0 + piece * PER;
+    const int piece = lane & 7, row0 = lane >> 3, col = piece * PER;
+    uint4 v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const int row = i * 4 + (lane >> 3);
-        uint4 v;
-        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+        const int row = i * 4 + row0;
+        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v[i].x), "=r"(v[i].y), "=r"(v[i].z), "=r"(v[i].w)
                      : "r"(block + (uint32_t)row * 128u + (((uint32_t)(piece ^ (row & 7))) << 4)) : "memory");
-        if (m0 + row >= live || col >= N) continue;
-        T* dst = out + (m0 + row) * ld + col;
-        if (vec && col + PER <= N) *reinterpret_cast<uint4*>(dst) = v;
-        else {
-            const T* e = reinterpret_cast<const T*>(&v);
+    }
+    T* dst = out + row0 * ld + col;
+    if (vec && rows == 32 && col + PER <= cols) {
 #pragma unroll
-            for (int j = 0; j < PER; ++j) if (col + j < N) dst[j] = e[j];
+        for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4*>(dst + (int64_t)(4 * i) * ld) = v[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (i * 4 + row0 >= rows) continue;
+            T* d = dst + (int64_t)(4 * i) * ld;
+            if (vec && col + PER <= cols) *reinterpret_cast<uint4*>(d) = v[i];
+            else {
+                const T* e = reinterpret_cast<const T*>(&v[i]);
+#pragma unroll
+                for (int j = 0; j < PER; ++j) if (col + j < cols) d[j] = e[j];
+            }
         }
     }
 }
 
+// A place in a ring of N and the parity of its current round.
+template <int N> struct Ring {
+    int at = 0;
+    uint32_t round = 0;
+    __device__ __forceinline__ void next() { if (++at == N) { at = 0; round ^= 1u; } }
+};
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+
 template <int BN, typename T>
 __global__ void __launch_bounds__(QP_THREADS, 1)
-q8_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const QpArgs g) {
+q8_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out, const QpArgs g) {
     using Cfg = QpCfg<BN>;
     constexpr int STAGES = Cfg::STAGES, ACCS = Cfg::ACCS, COLS = BN / 2;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t tiles = (raw + 1023u) & ~1023u;
     const uint32_t out_blocks = tiles + STAGES * Cfg::STAGE_BYTES;
-    const uint32_t bars = out_blocks + QP_EW * QP_OUT_BLOCK;
+    const uint32_t bars = out_blocks + QP_EW * 2 * QP_OUT_BLOCK;
     auto full_bar = [&](int s) { return bars + 8u * s; };
     auto empty_bar = [&](int s) { return bars + 8u * (STAGES + s); };
     auto acc_full = [&](int a) { return bars + 8u * (2 * STAGES + a); };
@@ -82,10 +119,10 @@ q8_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     volatile uint32_t* tmem_word_ptr = reinterpret_cast<volatile uint32_t*>(smem_raw + (tmem_word - raw));
     int32_t* err = g.status + 1;
 
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-        for (int a = 0; a < ACCS; ++a) { mbar_init(acc_full(a), 1); mbar_init(acc_empty(a), 32 * QP_EW); }
+        for (int a = 0; a < ACCS; ++a) { mbar_init(acc_full(a), 1); mbar_init(acc_empty(a), QP_EW); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("prefetch.tensormap [%0];" :: "l"(&map_a) : "memory");
         asm volatile("prefetch.tensormap [%0];" :: "l"(&map_b) : "memory");
@@ -98,28 +135,29 @@ q8_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem_base = *tmem_word_ptr;
+    const uint32_t tmem_base = __shfl_sync(0xffffffffu, *tmem_word_ptr, 0);
     wait_for_predecessor();
 
     int64_t live = g.n;
     if (g.d_n) { const int64_t d = *g.d_n; live = d < live ? (d < 0 ? 0 : d) : live; }
     const int kbs = (g.K + Q8_BLOCK - 1) / Q8_BLOCK;
-    const int64_t total = (live + TC_BM - 1) / TC_BM * g.n_tiles;
+    const uint32_t total = (uint32_t)((live + TC_BM - 1) / TC_BM) * (uint32_t)g.n_tiles, n_tiles = (uint32_t)g.n_tiles;
 
-    if (warp == 0) {
+    if (warp < 4) {
+        if (Cfg::SPLIT) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(QP_REGS_FEW));
         // ---------------- TMA producer
-        if (lane == 0) {
+        if (warp == 0 && lane == 0) {
+            Ring<STAGES> ring;
             uint32_t it = 0;
             bool ok = true;
-            for (int64_t t = blockIdx.x; t < total && ok; t += gridDim.x) {
-                const int nt = (int)(t % g.n_tiles), mt = (int)(t / g.n_tiles);      // the column tiles of a row tile side by side
-                for (int kb = 0; kb < kbs; ++kb, ++it) {
-                    const int s = it % STAGES;
-                    if (!(ok = mbar_wait(empty_bar(s), ((it / STAGES) & 1u) ^ 1u, err, 1))) break;
-                    const uint32_t a_dst = tiles + s * Cfg::STAGE_BYTES, b_dst = a_dst + Cfg::A_BYTES;
-                    mbar_expect_tx(full_bar(s), Cfg::STAGE_BYTES);
-                    tma_load_2d(a_dst, &map_a, full_bar(s), kb * Q8_BLOCK, mt * TC_BM);
-                    tma_load_2d(b_dst, &map_b, full_bar(s), kb * Q8_BLOCK, nt * BN);
+            for (uint32_t t = blockIdx.x; t < total && ok; t += gridDim.x) {
+                const int mt = (int)(t / n_tiles), nt = (int)(t - (uint32_t)mt * n_tiles);      // the column tiles of a row tile side by side
+                for (int kb = 0; kb < kbs; ++kb, ++it, ring.next()) {
+                    if (!(ok = mbar_wait(empty_bar(ring.at), ring.round ^ 1u, err, 1))) break;
+                    const uint32_t a_dst = tiles + ring.at * Cfg::STAGE_BYTES, b_dst = a_dst + Cfg::A_BYTES, bar = full_bar(ring.at);
+                    mbar_expect_tx(bar, Cfg::STAGE_BYTES);
+                    tma_load_2d(a_dst, &map_a, bar, kb * Q8_BLOCK, mt * TC_BM);
+                    tma_load_2d(b_dst, &map_b, bar, kb * Q8_BLOCK, nt * BN);
                 }
             }
             if (*reinterpret_cast<volatile int32_t*>(err) != 0) {
@@ -130,37 +168,49 @@ q8_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                         __nanosleep(64);
             }
         }
-    } else if (warp == 1) {
-        // ---------------- MMA issuer
-        if (lane == 0) {
+        // ---------------- MMA issuers: two warps, every second block of K each (blocks have accumulators of their own, so the order
+        // between the two does not matter).  To wait for two barriers and to issue takes 700 cycles from block to block, the
+        // products of 256 columns 512.  The whole warp walks the loop, so that what it counts stays in uniform registers; one lane issues.
+        if (warp == 1 || warp == 2) {
             constexpr uint32_t idesc = instr_desc_e4m3(BN);
-            uint32_t it = 0;
+            const uint64_t a_desc = smem_desc(tiles, 16, 1024), b_desc = smem_desc(tiles + Cfg::A_BYTES, 16, 1024);
+            Ring<STAGES> ring;
+            Ring<ACCS> acc;
+            uint32_t mine = (uint32_t)warp & 1u;
             bool ok = true;
-            for (int64_t t = blockIdx.x; t < total && ok; t += gridDim.x) {
-                for (int kb = 0; kb < kbs; ++kb, ++it) {
-                    const int s = it % STAGES, a = it % ACCS;
-                    if (!(ok = mbar_wait(acc_empty(a), ((it / ACCS) & 1u) ^ 1u, err, 2))) break;
-                    if (!(ok = mbar_wait(full_bar(s), (it / STAGES) & 1u, err, 3))) break;
+            for (uint32_t t = blockIdx.x; t < total && ok; t += gridDim.x) {
+                for (int kb = 0; kb < kbs; ++kb, ring.next(), acc.next(), mine ^= 1u) {
+                    if (!mine) continue;
+                    ok = mbar_wait(full_bar(ring.at), ring.round, err, 3) && mbar_wait(acc_empty(acc.at), acc.round ^ 1u, err, 2);
+                    if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
                     tc_fence_after();
-                    const uint32_t a_src = tiles + s * Cfg::STAGE_BYTES, b_src = a_src + Cfg::A_BYTES;
+                    const uint64_t step = (uint64_t)(uint32_t)(ring.at * (Cfg::STAGE_BYTES >> 4));      // (addresses in a descriptor are in 16 bytes)
+                    const uint32_t d = tmem_base + (uint32_t)(acc.at * BN);
+                    if (elect_one()) {
 #pragma unroll
-                    for (int k = 0; k < Q8_BLOCK / 32; ++k)
-                        tc_mma_f8(tmem_base + (uint32_t)(a * BN), smem_desc(a_src + k * 32, 16, 1024), smem_desc(b_src + k * 32, 16, 1024), idesc, k > 0 ? 1u : 0u);
-                    tc_commit(empty_bar(s));
-                    tc_commit(acc_full(a));
+                        for (int k = 0; k < Q8_BLOCK / 32; ++k) tc_mma_f8(d, a_desc + step + 2 * k, b_desc + step + 2 * k, idesc, k > 0 ? 1u : 0u);
+                        tc_commit(acc_full(acc.at));
+                        tc_commit(empty_bar(ring.at));
+                    }
+                    __syncwarp();
                 }
             }
         }
     } else {
+        if (Cfg::SPLIT) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(QP_REGS_MANY));
         // ---------------- epilogue warps
-        const int quarter = warp & 3, part = (warp - 2) >> 2;
-        const uint32_t block = out_blocks + (uint32_t)(warp - 2) * QP_OUT_BLOCK;
+        const int quarter = warp & 3, part = (warp - 4) >> 2;
+        const uint32_t block = out_blocks + (uint32_t)(warp - 4) * 2 * QP_OUT_BLOCK;
         const uint32_t t_lane = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(part * COLS);
-        uint32_t it = 0;
+        // an accumulator is read in pieces of 32 columns, the next one on its way while one is added up: also across accumulators
+        constexpr int WIDE = COLS >= 64 ? 32 : 16, PIECES = COLS / WIDE;
+        static_assert(PIECES % 2 == 0, "the first piece is always in r[0]");
+        Ring<ACCS> ring;
         bool ok = true;
-        for (int64_t t = blockIdx.x; t < total && ok; t += gridDim.x) {
-            const int nt = (int)(t % g.n_tiles);
-            const int64_t m0 = t / g.n_tiles * TC_BM + quarter * 32, m = m0 + lane;
+        for (uint32_t t = blockIdx.x; t < total && ok; t += gridDim.x) {
+            const uint32_t mt = t / n_tiles;
+            const int nt = (int)(t - mt * n_tiles);
+            const int64_t m0 = (int64_t)mt * TC_BM + quarter * 32, m = m0 + lane;
             const int n0 = nt * BN + part * COLS;
             const float* sa = m < live ? g.a_scale + m * kbs : nullptr;
             const float* sb = n0 < g.N ? g.b_scale + (int64_t)(n0 / Q8_BLOCK) * kbs : nullptr;
@@ -168,25 +218,36 @@ q8_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
 #pragma unroll
             for (int i = 0; i < COLS / 2; ++i) acc[i] = 0ull;
             float s_next = sa && sb ? __ldg(sa) * __ldg(sb) : 0.f;
-            for (int kb = 0; kb < kbs; ++kb, ++it) {
+            uint32_t r[2][WIDE];
+            ok = qp_warp_wait(acc_full(ring.at), ring.round, err, lane);
+            tc_fence_after();
+            if (ok) qp_ld(t_lane + (uint32_t)(ring.at * BN), r[0]);
+            for (int kb = 0; kb < kbs && ok; ++kb) {
                 const uint32_t s32 = __float_as_uint(s_next);
-                if (kb + 1 < kbs && sa && sb) s_next = __ldg(sa + kb + 1) * __ldg(sb + kb + 1);      // on its way during the wait
-                const int a = it % ACCS;
-                if (!(ok = mbar_wait(acc_full(a), (it / ACCS) & 1u, err, 4))) break;
-                __syncwarp();
-                tc_fence_after();
                 const uint64_t s2 = pair64(s32, s32);
-                uint32_t r[2][16];
-                tc_ld16(t_lane + (uint32_t)(a * BN), r[0]);
+                const bool more = kb + 1 < kbs;
+                if (more && sa && sb) s_next = __ldg(sa + kb + 1) * __ldg(sb + kb + 1);
+                const int a = ring.at;
+                ring.next();
 #pragma unroll
-                for (int c = 0; c < COLS / 16; ++c) {
+                for (int c = 0; c < PIECES; ++c) {
                     tc_wait_ld(r[c & 1]);
-                    if (c + 1 < COLS / 16) tc_ld16(t_lane + (uint32_t)(a * BN + (c + 1) * 16), r[(c + 1) & 1]);
-                    else { tc_fence_before(); mbar_arrive_relaxed(acc_empty(a)); }      // all of it has been read
+                    if (c + 1 < PIECES) qp_ld(t_lane + (uint32_t)(a * BN + (c + 1) * WIDE), r[(c + 1) & 1]);
+                    else {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_relaxed(acc_empty(a));      // all of it has been read (one arrival a warp: 256 took as long as the products)
+                        if (more) {
+                            ok = qp_warp_wait(acc_full(ring.at), ring.round, err, lane);
+                            tc_fence_after();
+                            qp_ld(t_lane + (uint32_t)(ring.at * BN), r[0]);
+                        }
+                    }
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) fma_pair(acc[c * 8 + i], pair64(r[c & 1][2 * i], r[c & 1][2 * i + 1]), s2);
+                    for (int i = 0; i < WIDE / 2; ++i) fma_pair(acc[c * (WIDE / 2) + i], pair64(r[c & 1][2 * i], r[c & 1][2 * i + 1]), s2);
                 }
             }
+            tc_wait_ld(r[0]);                                 // (nothing is on its way, unless a wait gave up)
             if (!ok) break;
             // a lane's row leaves in pieces of 128 bytes through the warp's block
             T* out = static_cast<T*>(g.out);
@@ -195,8 +256,10 @@ q8_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
 #pragma unroll
             for (int c = 0; c < (COLS + PIECE - 1) / PIECE; ++c) {
                 if (n0 + c * PIECE >= g.N) break;             // (uniform over the warp)
-                __syncwarp();                                 // the block's previous contents have been read
-                const uint32_t row = block + (uint32_t)lane * 128u;
+                const uint32_t box = block + (uint32_t)(c & 1) * QP_OUT_BLOCK;
+                if (lane == 0) tma_store_wait_read<1>();      // the block's previous contents have been read (a copy is one group)
+                __syncwarp();
+                const uint32_t row = box + (uint32_t)lane * 128u;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     uint32_t w[4] = {0u, 0u, 0u, 0u};
@@ -214,11 +277,21 @@ q8_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                     }
                     sts_u4(row + ((((uint32_t)j) ^ (uint32_t)(lane & 7)) << 4), make_uint4(w[0], w[1], w[2], w[3]));
                 }
-                __syncwarp();
-                const int edge = min(g.N, n0 + COLS);         // (of half a piece: the other half is another warp's)
-                qp_store_block<T>(block, out, g.ld_out, m0, live, n0 + c * PIECE, edge, g.vec != 0, lane);
+                const int rows = (int)min((int64_t)32, live - m0), cols = min(g.N, n0 + COLS) - (n0 + c * PIECE);     // (of half a piece: the other half is another warp's)
+                if (g.vec && COLS >= PIECE && rows > 0 && (rows == 32 || live == g.n)) {
+                    // the copy engine takes it from here and drops what lies past the edges
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) tma_store_2d(&map_out, box, n0 + c * PIECE, (int)m0);
+                } else {
+                    __syncwarp();
+                    if (rows > 0) qp_store_block<T>(box, out + m0 * g.ld_out + n0 + c * PIECE, g.ld_out, rows, cols, g.vec != 0, lane);
+                    __syncwarp();
+                    if (lane == 0) asm volatile("cp.async.bulk.commit_group;" ::: "memory");      // (an empty group, in the place of a copy's)
+                }
             }
         }
+        if (lane == 0) tma_store_wait_all();
     }
 
     tc_fence_before();
@@ -316,9 +389,12 @@ template <int BN, typename T> static cudaError_t qp_go(const Q8Args& q, cudaStre
     g.n_tiles = (int)ceil_div(q.N, BN);
     g.out = q.out; g.ld_out = q.ld_out; g.status = q.status;
     g.vec = (reinterpret_cast<uintptr_t>(q.out) & 15u) == 0 && (q.ld_out * (int64_t)sizeof(T)) % 16 == 0;
+    CUtensorMap mo = ma;
+    if (g.vec && !encode_map(&mo, TmaSpec{q.out, q.n, q.N, q.ld_out, 0, 1, 32, 128 / (int)sizeof(T), sizeof(T) == 4, 128})) return cudaErrorInvalidValue;
     const int64_t tiles = ceil_div(q.n, TC_BM) * g.n_tiles;
+    if (tiles > INT32_MAX) return cudaErrorInvalidValue;     // (an output of 2^31 tiles fits no memory)
     const int grid = tiles < sm_count() ? (int)tiles : sm_count();
-    return launch_dependent(kernel, dim3(grid), dim3(QP_THREADS), (size_t)Cfg::SMEM, st, ma, mb, g);
+    return launch_dependent(kernel, dim3(grid), dim3(QP_THREADS), (size_t)Cfg::SMEM, st, ma, mb, mo, g);
 }
 template <int R, typename T> static cudaError_t qf_go(const Q8Args& q, cudaStream_t st) {
     return launch_dependent(q8_few_rows_kernel<R, T>, dim3((unsigned)ceil_div(q.N, 4), (unsigned)ceil_div(q.n, R)), dim3(128), 0, st, q);
