@@ -8,6 +8,10 @@
 // type it came in, from its load to its output; a block of 128 columns belongs to one warp (to half a warp where lanes hold 16
 // bytes of bf16), so that its largest magnitude needs no shared memory.  Rows wider than the registers go through the kernels
 // at the end, which read them again from the L2.
+#include <string.h>
+
+#include <type_traits>
+
 #include "internal.h"
 #include "q8.cuh"
 
@@ -24,8 +28,9 @@ template <> struct Chunk<float, true> {
     __device__ __forceinline__ void zero() { v = make_float4(0.f, 0.f, 0.f, 0.f); }
     __device__ __forceinline__ void load(const float* p, int lane, int left) { if (lane * 4 < left) v = *reinterpret_cast<const float4*>(p + lane * 4); else zero(); }
     __device__ __forceinline__ void store(float* p, int lane, int left) const { if (lane * 4 < left) *reinterpret_cast<float4*>(p + lane * 4) = v; }
-    __device__ __forceinline__ void get(float (&f)[4]) const { f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w; }
-    __device__ __forceinline__ void set(const float (&f)[4]) { v = make_float4(f[0], f[1], f[2], f[3]); }
+    __device__ __forceinline__ void add(const Chunk& r) { v.x += r.v.x; v.y += r.v.y; v.z += r.v.z; v.w += r.v.w; }
+    __device__ __forceinline__ void get(f32x2 (&f)[2]) const { f[0] = pack2(v.x, v.y); f[1] = pack2(v.z, v.w); }
+    __device__ __forceinline__ void set(const f32x2 (&f)[2]) { v = make_float4(low(f[0]), high(f[0]), low(f[1]), high(f[1])); }
 };
 template <> struct Chunk<__nv_bfloat16, true> {
     static constexpr int E = 8, COLS = 256, Q = 128;
@@ -35,17 +40,12 @@ template <> struct Chunk<__nv_bfloat16, true> {
     __device__ __forceinline__ void zero() { v = make_uint4(0u, 0u, 0u, 0u); }
     __device__ __forceinline__ void load(const __nv_bfloat16* p, int lane, int left) { if (lane * 8 < left) v = *reinterpret_cast<const uint4*>(p + lane * 8); else zero(); }
     __device__ __forceinline__ void store(__nv_bfloat16* p, int lane, int left) const { if (lane * 8 < left) *reinterpret_cast<uint4*>(p + lane * 8) = v; }
-    __device__ __forceinline__ void get(float (&f)[8]) const {
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+    __device__ __forceinline__ void add(const Chunk& r) {      // (each sum rounded once)
+        asm("add.rn.bf16x2 %0, %0, %1;" : "+r"(v.x) : "r"(r.v.x)); asm("add.rn.bf16x2 %0, %0, %1;" : "+r"(v.y) : "r"(r.v.y));
+        asm("add.rn.bf16x2 %0, %0, %1;" : "+r"(v.z) : "r"(r.v.z)); asm("add.rn.bf16x2 %0, %0, %1;" : "+r"(v.w) : "r"(r.v.w));
     }
-    __device__ __forceinline__ void set(const float (&f)[8]) {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]); w[i] = *reinterpret_cast<const uint32_t*>(&h); }
-        v = make_uint4(w[0], w[1], w[2], w[3]);
-    }
+    __device__ __forceinline__ void get(f32x2 (&f)[4]) const { f[0] = from_bf16x2(v.x); f[1] = from_bf16x2(v.y); f[2] = from_bf16x2(v.z); f[3] = from_bf16x2(v.w); }
+    __device__ __forceinline__ void set(const f32x2 (&f)[4]) { v = make_uint4(to_bf16x2(f[0]), to_bf16x2(f[1]), to_bf16x2(f[2]), to_bf16x2(f[3])); }
 };
 template <typename T> struct Chunk<T, false> {
     static constexpr int E = 4, COLS = 128, Q = 128;
@@ -64,78 +64,109 @@ template <typename T> struct Chunk<T, false> {
 #pragma unroll
         for (int e = 0; e < 4; ++e) if (lane + 32 * e < left) p[lane + 32 * e] = v[e];
     }
-    __device__ __forceinline__ void get(float (&f)[4]) const {
+    __device__ __forceinline__ void add(const Chunk& r) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) f[e] = (float)v[e];
+        for (int e = 0; e < 4; ++e) v[e] = v[e] + r.v[e];
     }
-    __device__ __forceinline__ void set(const float (&f)[4]) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = (T)f[e];
-    }
+    __device__ __forceinline__ void get(f32x2 (&f)[2]) const { f[0] = pack2((float)v[0], (float)v[1]); f[1] = pack2((float)v[2], (float)v[3]); }
+    __device__ __forceinline__ void set(const f32x2 (&f)[2]) { v[0] = (T)low(f[0]); v[1] = (T)high(f[0]); v[2] = (T)low(f[1]); v[3] = (T)high(f[1]); }
 };
 
-// E values of a vector of weights (null: ones)
-template <bool VEC, int E> __device__ __forceinline__ void load_weight(const float* w, int lane, int left, float (&f)[E]) {
+__device__ __forceinline__ float half_of(f32x2 v, int e) { return e & 1 ? high(v) : low(v); }
+
+// A lane's values of a vector of weights (null: ones)
+template <bool VEC, int H> __device__ __forceinline__ void load_weight(const float* w, int lane, int left, f32x2 (&f)[H]) {
     if (w == nullptr) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) f[e] = 1.f;
+        for (int e = 0; e < H; ++e) f[e] = both(1.f);
     } else if (VEC) {
 #pragma unroll
-        for (int e = 0; e < E; e += 4) {
-            const float4 v = lane * E + e < left ? __ldg(reinterpret_cast<const float4*>(w + lane * E + e)) : make_float4(0.f, 0.f, 0.f, 0.f);
-            f[e] = v.x; f[e + 1] = v.y; f[e + 2] = v.z; f[e + 3] = v.w;
+        for (int e = 0; e < H; e += 2) {
+            const float4 v = lane * 2 * H + 2 * e < left ? __ldg(reinterpret_cast<const float4*>(w + lane * 2 * H + 2 * e)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            f[e] = pack2(v.x, v.y); f[e + 1] = pack2(v.z, v.w);
         }
     } else {
 #pragma unroll
-        for (int e = 0; e < E; ++e) f[e] = lane + 32 * e < left ? __ldg(w + lane + 32 * e) : 0.f;
+        for (int e = 0; e < H; ++e)
+            f[e] = pack2(lane + 64 * e < left ? __ldg(w + lane + 64 * e) : 0.f, lane + 64 * e + 32 < left ? __ldg(w + lane + 64 * e + 32) : 0.f);
     }
 }
 
-// E results of a lane to a row of `dtype`.  For GEAR_E4M3 also the scales of the chunk's blocks, scale[0] the first one's.  The
-// whole warp calls.
-template <bool VEC, int E> __device__ __forceinline__ void put_row(void* row, int col0, int lane, int left, int dtype, float* scale, const float (&h)[E]) {
-    if (dtype == GEAR_E4M3) {
-        uint32_t m = 0u;
+// The largest magnitude of the block that a lane's values belong to.  The whole warp calls.
+template <bool VEC, int H> __device__ __forceinline__ float block_largest(const f32x2 (&v)[H], int lane) {
+    float most = 0.f;
 #pragma unroll
-        for (int e = 0; e < E; ++e) m = max(m, q8_magnitude(h[e]));
-        constexpr int LANES = VEC && E == 8 ? 16 : 32;                // lanes that share a block
-        m = __reduce_max_sync(LANES == 32 ? 0xffffffffu : lane < 16 ? 0xffffu : 0xffff0000u, m);
-        float inv;
-        const float s = q8_scale(m, inv);
-        if (lane % LANES == 0 && (lane / LANES) * Q8_BLOCK < left) scale[lane / LANES] = s;
-        uint8_t* q = static_cast<uint8_t*>(row) + col0;
-        if (VEC) {
-            uint32_t w[E / 4];
+    for (int e = 0; e < H; ++e) most = q8_larger(most, low(v[e]), high(v[e]));
+    if (VEC && H == 4) return __uint_as_float(__reduce_max_sync(lane < 16 ? 0xffffu : 0xffff0000u, __float_as_uint(most)));      // half a warp a block
+    return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));
+}
+// A lane's values in e4m3 to a row; quotient: what becomes of a pair
+template <bool VEC, int H, typename Fn> __device__ __forceinline__ void put_q8(uint8_t* q, int lane, int left, const f32x2 (&v)[H], const Fn& quotient) {
+    uint32_t w[H / 2];
 #pragma unroll
-            for (int e = 0; e < E; e += 4) w[e / 4] = (uint32_t)q8_pair(h[e] * inv, h[e + 1] * inv) | (uint32_t)q8_pair(h[e + 2] * inv, h[e + 3] * inv) << 16;
-            if (lane * E < left) {
-                if (E == 4) *reinterpret_cast<uint32_t*>(q + lane * 4) = w[0];
-                else *reinterpret_cast<uint2*>(q + lane * 8) = make_uint2(w[0], w[E / 4 - 1]);
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < E; ++e) if (lane + 32 * e < left) q[lane + 32 * e] = q8_one(h[e] * inv);
+    for (int e = 0; e < H; e += 2) w[e / 2] = (uint32_t)q8_pair(quotient(v[e])) | (uint32_t)q8_pair(quotient(v[e + 1])) << 16;
+    if (VEC) {
+        if (lane * 2 * H < left) {
+            if (H == 2) *reinterpret_cast<uint32_t*>(q + lane * 4) = w[0];
+            else *reinterpret_cast<uint2*>(q + lane * 8) = make_uint2(w[0], w[H / 2 - 1]);
         }
-    } else if (dtype == GEAR_BF16) {
-        __nv_bfloat16* o = static_cast<__nv_bfloat16*>(row) + col0;
-        if (VEC) {
-            uint32_t w[E / 2];
+    } else {
 #pragma unroll
-            for (int e = 0; e < E; e += 2) { const __nv_bfloat162 p = __floats2bfloat162_rn(h[e], h[e + 1]); w[e / 2] = *reinterpret_cast<const uint32_t*>(&p); }
-            if (lane * E < left) {
-                if (E == 4) *reinterpret_cast<uint2*>(o + lane * 4) = make_uint2(w[0], w[1]);
-                else *reinterpret_cast<uint4*>(o + lane * 8) = make_uint4(w[0], w[1], w[E / 2 - 2], w[E / 2 - 1]);
+        for (int e = 0; e < 2 * H; ++e) if (lane + 32 * e < left) q[lane + 32 * e] = (uint8_t)(w[e / 4] >> (8 * (e % 4)));
+    }
+}
+// The piece's values before r is known, if its block is a usual one; returns the block's largest.
+template <bool VEC, int H> __device__ __forceinline__ float put_q8_early(void* row, int col0, int lane, int left, const f32x2 (&v)[H]) {
+    const float largest = block_largest<VEC>(v, lane);
+    if (q8_usual(largest)) put_q8<VEC>(static_cast<uint8_t*>(row) + col0, lane, left, v, Q8Quotient(largest));
+    return largest;
+}
+// The scales of the piece's blocks, once r is known (scale[0]: the first one's); value(v) gets the values again, where they have to be
+// written by the definition.
+template <bool VEC, int H, typename Fn> __device__ __forceinline__ void put_q8_late(void* row, int col0, int lane, int left, float* scale, float largest, float r, Fn&& value) {
+    constexpr int LANES = VEC && H == 4 ? 16 : 32;                    // lanes that share a block
+    float s = q8_over_448(largest) * r;
+    if (!q8_usual(largest, r)) {
+        f32x2 v[H];
+        value(v);
+        const Q8Plain plain(largest, r);
+        put_q8<VEC>(static_cast<uint8_t*>(row) + col0, lane, left, v, plain);
+        s = plain.scale;
+    }
+    if (lane % LANES == 0 && (lane / LANES) * Q8_BLOCK < left) scale[lane / LANES] = s;
+}
+
+// A lane's values, times r, to a row of fp32 or bf16.
+template <bool VEC, int H> __device__ __forceinline__ void put_row(void* row, int col0, int lane, int left, int dtype, float r, f32x2 (&h)[H]) {
+    const bool in = lane * 2 * H < left;                              // (VEC: all of the lane's values or none)
+#pragma unroll
+    for (int e = 0; e < H; ++e) h[e] = mul2(h[e], both(r));
+    if (dtype == GEAR_BF16) {
+        __nv_bfloat16* o = static_cast<__nv_bfloat16*>(row) + col0;
+        uint32_t w[H];
+#pragma unroll
+        for (int e = 0; e < H; ++e) w[e] = to_bf16x2(h[e]);
+        if (VEC) {
+            if (in) {
+                if (H == 2) *reinterpret_cast<uint2*>(o + lane * 4) = make_uint2(w[0], w[1]);
+                else *reinterpret_cast<uint4*>(o + lane * 8) = make_uint4(w[0], w[1], w[H - 2], w[H - 1]);
             }
         } else {
 #pragma unroll
-            for (int e = 0; e < E; ++e) if (lane + 32 * e < left) o[lane + 32 * e] = __float2bfloat16(h[e]);
+            for (int e = 0; e < 2 * H; ++e) if (lane + 32 * e < left) o[lane + 32 * e] = __ushort_as_bfloat16((unsigned short)(w[e / 2] >> (16 * (e % 2))));
         }
     } else {
         float* o = static_cast<float*>(row) + col0;
+        if (VEC) {
+            if (in)
 #pragma unroll
-        for (int e = 0; e < E; e += VEC ? 4 : 1) {
-            if (VEC) { if (lane * E + e < left) *reinterpret_cast<float4*>(o + lane * E + e) = make_float4(h[e], h[e + (VEC ? 1 : 0)], h[e + (VEC ? 2 : 0)], h[e + (VEC ? 3 : 0)]); }
-            else if (lane + 32 * e < left) o[lane + 32 * e] = h[e];
+                for (int e = 0; e < H; e += 2) *reinterpret_cast<float4*>(o + lane * 2 * H + 2 * e) = make_float4(low(h[e]), high(h[e]), low(h[e + 1]), high(h[e + 1]));
+        } else {
+#pragma unroll
+            for (int e = 0; e < H; ++e) {
+                if (lane + 64 * e < left) o[lane + 64 * e] = low(h[e]);
+                if (lane + 64 * e + 32 < left) o[lane + 64 * e + 32] = high(h[e]);
+            }
         }
     }
 }
@@ -157,87 +188,85 @@ template <typename T> __device__ __forceinline__ void* row_of_out(const NormArgs
     return static_cast<char*>(a.out) + k * a.ld_out * (a.out_dtype == GEAR_E4M3 ? 1 : a.out_dtype == GEAR_BF16 ? 2 : 4);
 }
 
-// v summed over the W warps that share a row; scratch: W values of that row.  (All warps of the block call.)
-template <int W> __device__ __forceinline__ float sum_over_row(float v, float* scratch, int part) {
+// v summed over the warps that share a row; scratch: a word for each.  (All warps of the block call.)
+__device__ __forceinline__ float sum_over_row(float v, float* scratch, int part, int warps) {
     v = warp_sum(v);
-    if (W == 1) return v;
     if ((threadIdx.x & 31) == 0) scratch[part] = v;
     __syncthreads();
     float t = 0.f;
-#pragma unroll
-    for (int w = 0; w < W; ++w) t += scratch[w];
+    for (int w = 0; w < warps; ++w) t += scratch[w];
     return t;
 }
 
-constexpr int NORM_WARPS = 4;                    // warps per block where a warp has a row of its own
+constexpr int NORM_ROWS = 4;                     // rows per block where a warp has a row of its own
 
-// W warps per row (1, or all eight of the block), C chunks per warp: chunk c of the row belongs to warp c % W.
-template <typename T, bool VEC, int W, int C>
-__global__ void __launch_bounds__(W == 1 ? 32 * NORM_WARPS : 32 * W)
+// A row to a warp (ONE) or to all warps of a block; C pieces of columns a warp: piece c * warps + part.
+template <typename T, bool VEC, bool ONE, int C>
+__global__ void __launch_bounds__(ONE ? 32 * NORM_ROWS : 256)
 rms_norm_kernel(const NormArgs a) {
     typedef Chunk<T, VEC> Ch;
-    constexpr int ROWS = W == 1 ? NORM_WARPS : 1;
-    __shared__ float scratch[W];
+    constexpr int H = Ch::E / 2;
+    __shared__ float scratch[8];
     wait_for_predecessor();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = W == 1 ? 0 : warp;
-    const int64_t k = (int64_t)blockIdx.x * ROWS + (W == 1 ? warp : 0);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = ONE ? 0 : warp, warps = ONE ? 1 : blockDim.x >> 5;
+    const int64_t k = ONE ? (int64_t)blockIdx.x * NORM_ROWS + warp : (int64_t)blockIdx.x;
     if (k >= live_rows(a)) return;               // (uniform over the warps of a row)
     const T* x = row_of_x<T>(a, k, lane == 0 && part == 0);
+    auto first = [&](int c) { return (c * warps + part) * Ch::COLS; };
     Ch y[C];
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-        const int col0 = (c * W + part) * Ch::COLS;
-        if (col0 < a.cols && x) y[c].load(x + col0, lane, a.cols - col0); else y[c].zero();
-    }
+    for (int c = 0; c < C; ++c) { if (x) y[c].load(x + first(c), lane, a.cols - first(c)); else y[c].zero(); }
     if (a.res) {
         const T* res = static_cast<const T*>(a.res) + k * a.ld_res;
+        Ch r[C];
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int col0 = (c * W + part) * Ch::COLS;
-            if (col0 >= a.cols) continue;
-            Ch r;
-            r.load(res + col0, lane, a.cols - col0);
-            float f[Ch::E], g[Ch::E];
-            y[c].get(f); r.get(g);
+        for (int c = 0; c < C; ++c) r[c].load(res + first(c), lane, a.cols - first(c));
 #pragma unroll
-            for (int e = 0; e < Ch::E; ++e) f[e] += g[e];
-            y[c].set(f);                         // the residual stream is kept in its own type; the norm is the kept sum's
-        }
-    }
-    float sum = 0.f;
-    if (a.normed) {
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            float f[Ch::E];
-            y[c].get(f);
-#pragma unroll
-            for (int e = 0; e < Ch::E; ++e) sum = fmaf(f[e], f[e], sum);
-        }
-        sum = sum_over_row<W>(sum, scratch, part);
+        for (int c = 0; c < C; ++c) y[c].add(r[c]);      // the residual stream is kept in its own type; the norm is the kept sum's
     }
     if (a.res_out) {
         T* o = static_cast<T*>(a.res_out) + k * a.ld_res_out;
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int col0 = (c * W + part) * Ch::COLS;
-            if (col0 < a.cols) y[c].store(o + col0, lane, a.cols - col0);
-        }
+        for (int c = 0; c < C; ++c) y[c].store(o + first(c), lane, a.cols - first(c));
     }
-    const float r = a.normed ? 1.0f / sqrtf(sum / (float)a.cols + a.eps) : 1.f;
     void* out = row_of_out<T>(a, k);
-    float* scale = a.scale ? a.scale + k * a.blocks : nullptr;
+    const bool q8 = a.out_dtype == GEAR_E4M3;
+    auto value = [&](int c, f32x2 (&v)[H]) {     // y times the weights
+        y[c].get(v);
+        if (a.weight) {
+            f32x2 w[H];
+            load_weight<VEC, H>(a.weight + first(c), lane, a.cols - first(c), w);
+#pragma unroll
+            for (int e = 0; e < H; ++e) v[e] = mul2(v[e], w[e]);
+        }
+    };
+    float largest[C];
+    f32x2 sum2 = 0ull;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        const int col0 = (c * W + part) * Ch::COLS;
-        if (col0 >= a.cols) continue;
-        float f[Ch::E], w[Ch::E];
-        y[c].get(f);
-        if (a.normed) {
-            load_weight<VEC, Ch::E>(a.weight ? a.weight + col0 : nullptr, lane, a.cols - col0, w);
+        if (first(c) >= a.cols) continue;
+        f32x2 v[H];
+        y[c].get(v);
 #pragma unroll
-            for (int e = 0; e < Ch::E; ++e) f[e] = f[e] * r * w[e];
+        for (int e = 0; e < H; ++e) sum2 = fma2(v[e], v[e], sum2);
+        if (q8) { value(c, v); largest[c] = put_q8_early<VEC, H>(out, first(c), lane, a.cols - first(c), v); }
+    }
+    float r = 1.f;
+    if (a.normed) {
+        float sum = low(sum2) + high(sum2);
+        sum = ONE ? warp_sum(sum) : sum_over_row(sum, scratch, part, warps);
+        r = 1.0f / sqrtf(sum / (float)a.cols + a.eps);
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int col0 = first(c);
+        if (col0 >= a.cols) continue;
+        if (q8) put_q8_late<VEC, H>(out, col0, lane, a.cols - col0, a.scale + k * a.blocks + col0 / Q8_BLOCK, largest[c], r, [&](f32x2 (&v)[H]) { value(c, v); });
+        else {
+            f32x2 v[H];
+            value(c, v);
+            put_row<VEC, H>(out, col0, lane, a.cols - col0, a.out_dtype, r, v);
         }
-        put_row<VEC, Ch::E>(out, col0, lane, a.cols - col0, a.out_dtype, scale + col0 / Q8_BLOCK, f);
     }
 }
 
@@ -255,151 +284,259 @@ rms_norm_wide_kernel(const NormArgs a) {
         const T* res = a.res ? static_cast<const T*>(a.res) + k * a.ld_res : nullptr;
         T* kept = a.res_out ? static_cast<T*>(a.res_out) + k * a.ld_res_out : nullptr;
         // y of a chunk; once it has been kept it is read from there (res_out may be what it was made from)
-        auto get = [&](int col0, bool from_kept, float (&f)[Ch::E]) {
+        auto get = [&](int col0, bool from_kept, f32x2 (&f)[Ch::E / 2]) {
             Ch y;
             if (from_kept) { y.load(kept + col0, lane, a.cols - col0); y.get(f); return; }
             if (x) y.load(x + col0, lane, a.cols - col0); else y.zero();
-            y.get(f);
             if (res) {
                 Ch r;
-                float g[Ch::E];
-                r.load(res + col0, lane, a.cols - col0); r.get(g);
-#pragma unroll
-                for (int e = 0; e < Ch::E; ++e) f[e] += g[e];
-                y.set(f); y.get(f);
+                r.load(res + col0, lane, a.cols - col0);
+                y.add(r);
             }
+            y.get(f);
             if (kept) y.store(kept + col0, lane, a.cols - col0);
         };
-        float sum = 0.f;
+        f32x2 sum2 = 0ull;
         if (a.normed || kept)
             for (int col0 = part * Ch::COLS; col0 < a.cols; col0 += 8 * Ch::COLS) {
-                float f[Ch::E];
+                f32x2 f[Ch::E / 2];
                 get(col0, false, f);
 #pragma unroll
-                for (int e = 0; e < Ch::E; ++e) sum = fmaf(f[e], f[e], sum);
+                for (int e = 0; e < Ch::E / 2; ++e) sum2 = fma2(f[e], f[e], sum2);
             }
-        sum = sum_over_row<8>(sum, scratch, part);
+        const float sum = sum_over_row(low(sum2) + high(sum2), scratch, part, 8);
         const float r = a.normed ? 1.0f / sqrtf(sum / (float)a.cols + a.eps) : 1.f;
         void* out = row_of_out<T>(a, k);
-        float* scale = a.scale ? a.scale + k * a.blocks : nullptr;
         for (int col0 = part * Ch::COLS; col0 < a.cols; col0 += 8 * Ch::COLS) {
-            float f[Ch::E], w[Ch::E];
-            get(col0, kept != nullptr, f);
-            if (a.normed) {
-                load_weight<false, Ch::E>(a.weight ? a.weight + col0 : nullptr, lane, a.cols - col0, w);
+            constexpr int H = Ch::E / 2;
+            auto value = [&](f32x2 (&v)[H]) {
+                get(col0, kept != nullptr, v);
+                if (a.weight) {
+                    f32x2 w[H];
+                    load_weight<false, H>(a.weight + col0, lane, a.cols - col0, w);
 #pragma unroll
-                for (int e = 0; e < Ch::E; ++e) f[e] = f[e] * r * w[e];
-            }
-            put_row<false, Ch::E>(out, col0, lane, a.cols - col0, a.out_dtype, scale + col0 / Q8_BLOCK, f);
+                    for (int e = 0; e < H; ++e) v[e] = mul2(v[e], w[e]);
+                }
+            };
+            f32x2 v[H];
+            value(v);
+            if (a.out_dtype == GEAR_E4M3) {
+                const float largest = put_q8_early<false, H>(out, col0, lane, a.cols - col0, v);
+                put_q8_late<false, H>(out, col0, lane, a.cols - col0, a.scale + k * a.blocks + col0 / Q8_BLOCK, largest, r, value);
+            } else put_row<false, H>(out, col0, lane, a.cols - col0, a.out_dtype, r, v);
         }
         __syncthreads();                         // scratch is free for the next row
     }
 }
 
 // ---------------------------------------------------------------- gradients
-// Blocks walk the rows (of stripes one grid apart); a lane adds up its columns' part of dw in registers.  At the end the warps of a
-// block with a row each add theirs up in shared memory, one after the other, and the block's sums go to its row of `parts`: the
-// order is the same in every run.
-template <typename T, bool VEC, int W, int C>
-__global__ void __launch_bounds__(W == 1 ? 32 * NORM_WARPS : 32 * W)
+// A block has R rows at a time, a lane the same C pieces of their columns in all of them: it keeps its weights and its part of dw in
+// registers for as long as it lives, and the rows' sums take one meeting of the block's warps for R rows.  At the end the block's part
+// of dw goes to its row of `parts`.  Nothing is added up in an order that could change.
+// (A row to each warp: 172 registers in bf16, 741 us for 131072 rows of 1536; a block to each row, 504.)
+template <typename T, bool VEC, int C, int R, int PER_SM>
+__global__ void __launch_bounds__(256, PER_SM)
 rms_norm_back_kernel(const NormArgs a) {
     typedef Chunk<T, VEC> Ch;
-    constexpr int ROWS = W == 1 ? NORM_WARPS : 1;
-    __shared__ float scratch[2][2][W];
-    extern __shared__ float dw_sum[];            // W == 1: [cols]
+    __shared__ float scratch[2][8][2 * R];       // two sets in turn: a turn's sums are read by all before those of the turn after the next are written
     wait_for_predecessor();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = W == 1 ? 0 : warp;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     const int64_t live = live_rows(a);
     const float inv_cols = 1.0f / (float)a.cols;
-    float dw[C][Ch::E];
+    f32x2 w[C][Ch::E / 2], dw[C][Ch::E / 2];
+    int left[C];                                 // columns from the piece's first one on
 #pragma unroll
-    for (int c = 0; c < C; ++c)
+    for (int c = 0; c < C; ++c) {
+        const int col0 = (c * warps + warp) * Ch::COLS;
+        left[c] = a.cols - col0;
+        load_weight<VEC, Ch::E / 2>(a.weight && left[c] > 0 ? a.weight + col0 : nullptr, lane, left[c], w[c]);
 #pragma unroll
-        for (int e = 0; e < Ch::E; ++e) dw[c][e] = 0.f;
+        for (int e = 0; e < Ch::E / 2; ++e) dw[c][e] = 0ull;
+    }
     int odd = 0;
-    for (int64_t k = (int64_t)blockIdx.x * ROWS + (W == 1 ? warp : 0); k < live; k += (int64_t)gridDim.x * ROWS, odd ^= 1) {
-        const T* x = row_of_x<T>(a, k, lane == 0 && part == 0);
-        const T* dout = static_cast<const T*>(a.dout) + k * a.ld_dout;
-        Ch y[C], g[C];
-        float sq = 0.f, dot = 0.f;
+    for (int64_t k0 = (int64_t)blockIdx.x * R; k0 < live; k0 += (int64_t)gridDim.x * R, odd ^= 1) {
+        Ch y[R][C], g[R][C], s[R][C];
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int col0 = (c * W + part) * Ch::COLS;
-            if (col0 < a.cols) { if (x) y[c].load(x + col0, lane, a.cols - col0); else y[c].zero(); g[c].load(dout + col0, lane, a.cols - col0); }
-            else { y[c].zero(); g[c].zero(); }
-        }
+        for (int i = 0; i < R; ++i) {
+            const int64_t k = k0 + i;
+            const T* x = k < live ? row_of_x<T>(a, k, threadIdx.x == 0) : nullptr;
+            const T* dout = k < live ? static_cast<const T*>(a.dout) + k * a.ld_dout : nullptr;
+            const T* dres = k < live && a.dres ? static_cast<const T*>(a.dres) + k * a.ld_dres : nullptr;
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int col0 = (c * W + part) * Ch::COLS;
-            if (col0 >= a.cols) continue;
-            float f[Ch::E], d[Ch::E], w[Ch::E];
-            y[c].get(f); g[c].get(d);
-            load_weight<VEC, Ch::E>(a.weight ? a.weight + col0 : nullptr, lane, a.cols - col0, w);
-#pragma unroll
-            for (int e = 0; e < Ch::E; ++e) { sq = fmaf(f[e], f[e], sq); dot = fmaf(d[e] * w[e], f[e], dot); }
-        }
-        // (two sets of scratch words in turn: a row's sums are read by all before the row after the next one's are written)
-        sq = warp_sum(sq); dot = warp_sum(dot);
-        if (W > 1) {
-            if (lane == 0) { scratch[odd][0][part] = sq; scratch[odd][1][part] = dot; }
-            __syncthreads();
-            sq = dot = 0.f;
-#pragma unroll
-            for (int w = 0; w < W; ++w) { sq += scratch[odd][0][w]; dot += scratch[odd][1][w]; }
-        }
-        const float r = 1.0f / sqrtf(sq * inv_cols + a.eps);
-        const float q = r * r * (dot * inv_cols);          // dx = r (g - y q): r alone may be large where y is small
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int col0 = (c * W + part) * Ch::COLS;
-            if (col0 >= a.cols) continue;
-            float f[Ch::E], d[Ch::E], w[Ch::E];
-            y[c].get(f); g[c].get(d);
-            if (a.dx) {
-                load_weight<VEC, Ch::E>(a.weight ? a.weight + col0 : nullptr, lane, a.cols - col0, w);
-                float o[Ch::E];
-#pragma unroll
-                for (int e = 0; e < Ch::E; ++e) o[e] = r * (d[e] * w[e] - f[e] * q);
-                if (a.dres) {
-                    Ch s;
-                    float t[Ch::E];
-                    s.load(static_cast<const T*>(a.dres) + k * a.ld_dres + col0, lane, a.cols - col0);
-                    s.get(t);
-#pragma unroll
-                    for (int e = 0; e < Ch::E; ++e) o[e] += t[e];
-                }
-                Ch s;
-                s.set(o);
-                s.store(static_cast<T*>(a.dx) + k * a.ld_dx + col0, lane, a.cols - col0);
+            for (int c = 0; c < C; ++c) {
+                const int col0 = (c * warps + warp) * Ch::COLS;
+                if (x) y[i][c].load(x + col0, lane, left[c]); else y[i][c].zero();
+                if (dout) g[i][c].load(dout + col0, lane, left[c]); else g[i][c].zero();
+                if (dres) s[i][c].load(dres + col0, lane, left[c]); else s[i][c].zero();
             }
+        }
+        float sum[2 * R];
 #pragma unroll
-            for (int e = 0; e < Ch::E; ++e) dw[c][e] = fmaf(d[e] * r, f[e], dw[c][e]);
+        for (int i = 0; i < R; ++i) {
+            f32x2 sq = 0ull, dot = 0ull;
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                f32x2 f[Ch::E / 2], d[Ch::E / 2];
+                y[i][c].get(f); g[i][c].get(d);
+#pragma unroll
+                for (int e = 0; e < Ch::E / 2; ++e) { sq = fma2(f[e], f[e], sq); dot = fma2(mul2(d[e], w[c][e]), f[e], dot); }
+            }
+            sum[2 * i] = warp_sum(low(sq) + high(sq)); sum[2 * i + 1] = warp_sum(low(dot) + high(dot));
+        }
+        if (warps > 1) {
+#pragma unroll
+            for (int i = 0; i < 2 * R; ++i) if (lane == i) scratch[odd][warp][i] = sum[i];
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < 2 * R; ++i) sum[i] = 0.f;
+            for (int v = 0; v < warps; ++v)
+#pragma unroll
+                for (int i = 0; i < 2 * R; ++i) sum[i] += scratch[odd][v][i];
+        }
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const int64_t k = k0 + i;
+            if (k >= live) continue;
+            const float r = 1.0f / sqrtf(sum[2 * i] * inv_cols + a.eps);
+            const float q = r * r * (sum[2 * i + 1] * inv_cols);          // dx = r (g - y q): r alone may be large where y is small
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                f32x2 f[Ch::E / 2], d[Ch::E / 2], o[Ch::E / 2];
+                y[i][c].get(f); g[i][c].get(d); s[i][c].get(o);
+#pragma unroll
+                for (int e = 0; e < Ch::E / 2; ++e) {
+                    o[e] = fma2(both(r), fma2(f[e], both(-q), mul2(d[e], w[c][e])), o[e]);
+                    dw[c][e] = fma2(mul2(d[e], both(r)), f[e], dw[c][e]);
+                }
+                if (a.dx) {
+                    s[i][c].set(o);
+                    s[i][c].store(static_cast<T*>(a.dx) + k * a.ld_dx + (c * warps + warp) * Ch::COLS, lane, left[c]);
+                }
+            }
         }
     }
     if (!a.parts) return;
     float* to = a.parts + (int64_t)blockIdx.x * a.cols;
-    if (W == 1) {
-        for (int turn = 0; turn < ROWS; ++turn) {
-            if (warp == turn)
 #pragma unroll
-                for (int c = 0; c < C; ++c)
+    for (int c = 0; c < C; ++c)
 #pragma unroll
-                    for (int e = 0; e < Ch::E; ++e) {
-                        const int col = c * Ch::COLS + Ch::col(lane, e);
-                        if (col < a.cols) dw_sum[col] = turn == 0 ? dw[c][e] : dw_sum[col] + dw[c][e];
-                    }
-            __syncthreads();
-        }
-        for (int col = threadIdx.x; col < a.cols; col += 32 * NORM_WARPS) to[col] = dw_sum[col];
-    } else {
+        for (int e = 0; e < Ch::E; ++e) if (Ch::in(lane, e, left[c])) to[(c * warps + warp) * Ch::COLS + Ch::col(lane, e)] = half_of(dw[c][e / 2], e);
+}
+
+// A warp has rows of its own, one grid's warps apart, and STREAM - 1 of them on their way into shared memory while it works on one: a
+// lane copies (16 bytes at a time) the very pieces it will read, so that nobody waits for anybody.  A kernel that loads a row,
+// computes and stores keeps too little in flight: 262144 rows of 1536 in bf16 with a residual took 556 us with a row to a warp and 612
+// with a row to a block.
+constexpr int STREAM = 2, STREAM_WARPS = 4;
+constexpr int stream_smem(int arrays, int C) { return STREAM_WARPS * STREAM * arrays * C * 512; }
+
+// The pieces of row `row` (null: zeros) to the lane's places at `smem`.
+template <typename T, int C> __device__ __forceinline__ void stream_row(uint32_t smem, const T* row, const T* any, int lane, int cols) {
+    constexpr int E = 16 / (int)sizeof(T);
 #pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int e = 0; e < Ch::E; ++e) {
-                const int col = (c * W + part) * Ch::COLS + Ch::col(lane, e);
-                if (col < a.cols) to[col] = dw[c][e];
-            }
+    for (int c = 0; c < C; ++c) {
+        const int col = c * 32 * E + lane * E;
+        const bool there = row != nullptr && col < cols;
+        cp_async_16(smem + (uint32_t)(c * 512 + lane * 16), there ? row + col : any, there ? 16 : 0);
     }
+}
+template <typename T, typename Ch> __device__ __forceinline__ void take_piece(Ch& ch, uint32_t smem, int c, int lane) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(smem + (uint32_t)(c * 512 + lane * 16)) : "memory");
+    memcpy(&ch.v, &v, 16);
+}
+
+// A row is read from shared memory twice (sums, results), so
+// that registers hold little but the warp's part of dw; at the end the warps of a block add theirs up one after the other.
+template <typename T, int C, bool RES>
+__global__ void __launch_bounds__(32 * STREAM_WARPS)
+rms_norm_back_stream_kernel(const NormArgs a) {
+    typedef Chunk<T, true> Ch;
+    constexpr int ARRAYS = RES ? 3 : 2;
+    extern __shared__ __align__(16) uint8_t stream_mem[];
+    wait_for_predecessor();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t mine = (uint32_t)__cvta_generic_to_shared(stream_mem) + (uint32_t)(warp * STREAM * ARRAYS * C * 512);
+    const int64_t live = live_rows(a), step = (int64_t)gridDim.x * STREAM_WARPS;
+    const T *any = static_cast<const T*>(a.x), *dout = static_cast<const T*>(a.dout), *dres = static_cast<const T*>(a.dres);
+    const float inv_cols = 1.0f / (float)a.cols;
+    int64_t next = (int64_t)blockIdx.x * STREAM_WARPS + warp;
+    int next_slot = 0;
+    auto send = [&] {
+        if (next < live) {
+            const uint32_t at = mine + (uint32_t)(next_slot * ARRAYS * C * 512);
+            stream_row<T, C>(at, row_of_x<T>(a, next, lane == 0), any, lane, a.cols);
+            stream_row<T, C>(at + C * 512, dout + next * a.ld_dout, dout, lane, a.cols);
+            if (RES) stream_row<T, C>(at + 2 * C * 512, dres + next * a.ld_dres, dres, lane, a.cols);
+        }
+        cp_async_commit();
+        next += step;
+        next_slot = next_slot == STREAM - 1 ? 0 : next_slot + 1;
+    };
+    f32x2 dw[C][Ch::E / 2];
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int e = 0; e < Ch::E / 2; ++e) dw[c][e] = 0ull;
+    for (int d = 0; d < STREAM - 1; ++d) send();
+    int slot = 0;
+    for (int64_t k = (int64_t)blockIdx.x * STREAM_WARPS + warp; k < live; k += step) {
+        send();
+        cp_async_wait<STREAM - 1>();
+        const uint32_t at = mine + (uint32_t)(slot * ARRAYS * C * 512);
+        slot = slot == STREAM - 1 ? 0 : slot + 1;
+        f32x2 sq2 = 0ull, dot2 = 0ull;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            if (c * Ch::COLS >= a.cols) continue;
+            Ch y, g;
+            f32x2 f[Ch::E / 2], d[Ch::E / 2], w[Ch::E / 2];
+            take_piece<T>(y, at, c, lane); take_piece<T>(g, at + C * 512, c, lane);
+            y.get(f); g.get(d);
+            load_weight<true, Ch::E / 2>(a.weight ? a.weight + c * Ch::COLS : nullptr, lane, a.cols - c * Ch::COLS, w);
+#pragma unroll
+            for (int e = 0; e < Ch::E / 2; ++e) { sq2 = fma2(f[e], f[e], sq2); dot2 = fma2(mul2(d[e], w[e]), f[e], dot2); }
+        }
+        const float sq = warp_sum(low(sq2) + high(sq2)), dot = warp_sum(low(dot2) + high(dot2));
+        const float r = 1.0f / sqrtf(sq * inv_cols + a.eps);
+        const float q = r * r * (dot * inv_cols);
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int left = a.cols - c * Ch::COLS;
+            if (left <= 0) continue;
+            Ch y, g, s;
+            f32x2 f[Ch::E / 2], d[Ch::E / 2], w[Ch::E / 2], o[Ch::E / 2];
+            take_piece<T>(y, at, c, lane); take_piece<T>(g, at + C * 512, c, lane);
+            if (RES) take_piece<T>(s, at + 2 * C * 512, c, lane); else s.zero();
+            y.get(f); g.get(d); s.get(o);
+            load_weight<true, Ch::E / 2>(a.weight ? a.weight + c * Ch::COLS : nullptr, lane, left, w);
+#pragma unroll
+            for (int e = 0; e < Ch::E / 2; ++e) {
+                o[e] = fma2(both(r), fma2(f[e], both(-q), mul2(d[e], w[e])), o[e]);
+                dw[c][e] = fma2(mul2(d[e], both(r)), f[e], dw[c][e]);
+            }
+            if (a.dx) {
+                s.set(o);
+                s.store(static_cast<T*>(a.dx) + k * a.ld_dx + c * Ch::COLS, lane, left);
+            }
+        }
+    }
+    cp_async_wait<0>();
+    if (!a.parts) return;
+    float* sum = reinterpret_cast<float*>(stream_mem);
+    for (int turn = 0; turn < STREAM_WARPS; ++turn) {
+        __syncthreads();
+        if (warp == turn)
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int e = 0; e < Ch::E; ++e) {
+                    const int col = c * Ch::COLS + Ch::col(lane, e);
+                    if (col < a.cols) sum[col] = turn == 0 ? half_of(dw[c][e / 2], e) : sum[col] + half_of(dw[c][e / 2], e);
+                }
+    }
+    __syncthreads();
+    for (int col = threadIdx.x; col < a.cols; col += 32 * STREAM_WARPS) a.parts[(int64_t)blockIdx.x * a.cols + col] = sum[col];
 }
 
 // Rows of any width: two passes over a row; dw is added up in the block's row of `parts`, which belongs to it alone.
@@ -420,32 +557,33 @@ rms_norm_back_wide_kernel(const NormArgs a) {
         const T* x = row_of_x<T>(a, k, threadIdx.x == 0);
         const T* dout = static_cast<const T*>(a.dout) + k * a.ld_dout;
         float sq = 0.f, dot = 0.f;
+        f32x2 sq2 = 0ull, dot2 = 0ull;
         for (int pass = 0; pass < 2; ++pass) {
             const float inv_cols = 1.0f / (float)a.cols;
             const float r = 1.0f / sqrtf(sq * inv_cols + a.eps), q = r * r * (dot * inv_cols);      // (second pass)
             for (int col0 = part * Ch::COLS; col0 < a.cols; col0 += 8 * Ch::COLS) {
                 const int left = a.cols - col0;
                 Ch y, g;
-                float f[Ch::E], d[Ch::E], w[Ch::E], o[Ch::E];
+                f32x2 f[Ch::E / 2], d[Ch::E / 2], w[Ch::E / 2], o[Ch::E / 2];
                 if (x) y.load(x + col0, lane, left); else y.zero();
                 g.load(dout + col0, lane, left);
                 y.get(f); g.get(d);
-                load_weight<false, Ch::E>(a.weight ? a.weight + col0 : nullptr, lane, left, w);
+                load_weight<false, Ch::E / 2>(a.weight ? a.weight + col0 : nullptr, lane, left, w);
                 if (pass == 0) {
 #pragma unroll
-                    for (int e = 0; e < Ch::E; ++e) { sq = fmaf(f[e], f[e], sq); dot = fmaf(d[e] * w[e], f[e], dot); }
+                    for (int e = 0; e < Ch::E / 2; ++e) { sq2 = fma2(f[e], f[e], sq2); dot2 = fma2(mul2(d[e], w[e]), f[e], dot2); }
                     continue;
                 }
                 if (a.dx) {
 #pragma unroll
-                    for (int e = 0; e < Ch::E; ++e) o[e] = r * (d[e] * w[e] - f[e] * q);
+                    for (int e = 0; e < Ch::E / 2; ++e) o[e] = mul2(both(r), fma2(f[e], both(-q), mul2(d[e], w[e])));
                     Ch s;
                     if (a.dres) {
-                        float t[Ch::E];
+                        f32x2 t[Ch::E / 2];
                         s.load(static_cast<const T*>(a.dres) + k * a.ld_dres + col0, lane, left);
                         s.get(t);
 #pragma unroll
-                        for (int e = 0; e < Ch::E; ++e) o[e] += t[e];
+                        for (int e = 0; e < Ch::E / 2; ++e) o[e] = add2(o[e], t[e]);
                     }
                     s.set(o);
                     s.store(static_cast<T*>(a.dx) + k * a.ld_dx + col0, lane, left);
@@ -453,76 +591,113 @@ rms_norm_back_wide_kernel(const NormArgs a) {
                 if (to)
 #pragma unroll
                     for (int e = 0; e < Ch::E; ++e)
-                        if (Ch::in(lane, e, left)) { float* p = to + col0 + Ch::col(lane, e); *p = fmaf(d[e] * r, f[e], *p); }
+                        if (Ch::in(lane, e, left)) { float* p = to + col0 + Ch::col(lane, e); *p = fmaf(half_of(d[e / 2], e) * r, half_of(f[e / 2], e), *p); }
             }
-            if (pass == 0) { sq = sum_over_row<8>(sq, scratch[0], part); dot = sum_over_row<8>(dot, scratch[1], part); }
+            if (pass == 0) { sq = sum_over_row(low(sq2) + high(sq2), scratch[0], part, 8); dot = sum_over_row(low(dot2) + high(dot2), scratch[1], part, 8); }
         }
         __syncthreads();
     }
 }
 
-// dw[c] = the blocks' sums added up, always in the same order: 32 columns a block, eight warps over the rows
-__global__ void __launch_bounds__(256)
+// dw[c] = the blocks' sums added up, always in the same order: 32 columns a block, 32 warps over the rows, eight rows on their way
+// at a time (with eight warps and one row: as long as the rest of the call for 3001 rows of 1001)
+__global__ void __launch_bounds__(1024)
 norm_dweight_kernel(const float* __restrict__ parts, int rows, int cols, float* __restrict__ dweight) {
-    __shared__ float s[8][33];
+    __shared__ float s[32][33];
     wait_for_predecessor();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
     float t = 0.f;
-    if (col < cols) for (int r = warp; r < rows; r += 8) t += __ldcg(parts + (int64_t)r * cols + col);
+    if (col < cols)
+        for (int r0 = warp; r0 < rows; r0 += 32 * 8) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = r0 + 32 * i < rows ? __ldcg(parts + (int64_t)(r0 + 32 * i) * cols + col) : 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) t += v[i];
+        }
     s[warp][lane] = t;
     __syncthreads();
-    if (warp == 0 && col < cols) {
-        t = 0.f;
-        for (int w = 0; w < 8; ++w) t += s[w][lane];
-        dweight[col] = t;
-    }
+    t = warp_sum(s[lane][warp]);                 // warp w adds up column w
+    if (lane == 0 && blockIdx.x * 32 + warp < cols) dweight[blockIdx.x * 32 + warp] = t;
 }
 
 // ---------------------------------------------------------------- weights
-// One block per 128 x 128 weights: the block's values in shared memory (rows of 129 words, so that a warp may walk them in both
-// directions), their largest magnitude, both copies written in whole rows of the block.
-__global__ void __launch_bounds__(256)
-q8_weights_kernel(const float* __restrict__ W, int64_t ldw, int K, int N, uint8_t* __restrict__ q, int64_t ldq, float* __restrict__ scale,
+// One block per 128 x 128 weights.  A lane holds squares of 4 x 4 of them from their load on: its values of a row are four bytes of the
+// transposed copy, and, turned round in registers, four bytes of a column go to shared memory, from where whole rows of the other copy
+// leave.  (The weights as fp32 in shared memory, bytes stored one by one: 10.1 us for 2048 x 1024, this 4.)
+constexpr int QW_THREADS = 512;
+__device__ __forceinline__ void put_bytes(uint8_t* p, uint32_t w, int left, bool words) {
+    if (words && left >= 4) *reinterpret_cast<uint32_t*>(p) = w;
+    else
+        for (int i = 0; i < 4 && i < left; ++i) p[i] = (uint8_t)(w >> (8 * i));
+}
+__global__ void __launch_bounds__(QW_THREADS)
+q8_weights_kernel(const float* __restrict__ W, int64_t ldw, int vec, int K, int N, uint8_t* __restrict__ q, int64_t ldq, float* __restrict__ scale,
                   uint8_t* __restrict__ qt, int64_t ldqt, float* __restrict__ scale_t) {
-    extern __shared__ float tile[];              // [128][129]
-    __shared__ uint32_t most[8];
+    __shared__ uint32_t turned[Q8_BLOCK][33];    // [column][four rows]
+    __shared__ uint32_t most[QW_THREADS / 32];
     wait_for_predecessor();
+    constexpr int SQUARES = Q8_BLOCK / 4 / (QW_THREADS / 32);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int k0 = blockIdx.x * Q8_BLOCK, n0 = blockIdx.y * Q8_BLOCK, kn = min(Q8_BLOCK, K - k0), nn = min(Q8_BLOCK, N - n0);
-    uint32_t m = 0u;
-    for (int k = warp; k < kn; k += 8) {
-        const float* row = W + (int64_t)(k0 + k) * ldw + n0;
+    float4 v[SQUARES][4];
+    float mine = 0.f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int n = lane + 32 * e;
-            if (n >= nn) continue;
-            const float v = __ldg(row + n);
-            tile[k * 129 + n] = v;
-            m = max(m, q8_magnitude(v));
+    for (int i = 0; i < SQUARES; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int k = 4 * (warp + i * (QW_THREADS / 32)) + r, n = 4 * lane;
+            const float* p = W + (int64_t)(k0 + k) * ldw + n0 + n;
+            float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (k < kn) {
+                if (vec && n + 4 <= nn) f = __ldg(reinterpret_cast<const float4*>(p));
+                else {
+                    if (n < nn) f.x = __ldg(p);
+                    if (n + 1 < nn) f.y = __ldg(p + 1);
+                    if (n + 2 < nn) f.z = __ldg(p + 2);
+                    if (n + 3 < nn) f.w = __ldg(p + 3);
+                }
+            }
+            v[i][r] = f;
         }
-    }
-    m = __reduce_max_sync(0xffffffffu, m);
+#pragma unroll
+    for (int i = 0; i < SQUARES; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) mine = q8_larger(q8_larger(mine, v[i][r].x, v[i][r].y), v[i][r].z, v[i][r].w);
+    uint32_t m = __reduce_max_sync(0xffffffffu, __float_as_uint(mine));
     if (lane == 0) most[warp] = m;
     __syncthreads();
-    for (int w = 0; w < 8; ++w) m = max(m, most[w]);
-    float inv;
-    const float s = q8_scale(m, inv);
+    m = __reduce_max_sync(0xffffffffu, most[lane & (QW_THREADS / 32 - 1)]);
+    const float largest = __uint_as_float(m);
+    const bool usual = q8_usual(largest, 1.f);
+    const Q8Quotient fast(largest);
+    const Q8Plain plain(largest, 1.f);
     if (threadIdx.x == 0) {
+        const float s = usual ? fast.s : plain.scale;
         if (q) scale[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = s;
         if (qt) scale_t[(int64_t)blockIdx.x * gridDim.y + blockIdx.y] = s;
     }
-    if (q)
-        for (int n = warp; n < nn; n += 8) {
-            uint8_t* row = q + (int64_t)(n0 + n) * ldq + k0;
+    const bool words_t = (reinterpret_cast<uintptr_t>(qt) & 3u) == 0 && (ldqt & 3) == 0, words = (reinterpret_cast<uintptr_t>(q) & 3u) == 0 && (ldq & 3) == 0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) if (lane + 32 * e < kn) row[lane + 32 * e] = q8_one(tile[(lane + 32 * e) * 129 + n] * inv);
-        }
-    if (qt)
-        for (int k = warp; k < kn; k += 8) {
-            uint8_t* row = qt + (int64_t)(k0 + k) * ldqt + n0;
+    for (int i = 0; i < SQUARES; ++i) {
+        const int k4 = warp + i * (QW_THREADS / 32);
+        uint32_t w[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) if (lane + 32 * e < nn) row[lane + 32 * e] = q8_one(tile[k * 129 + lane + 32 * e] * inv);
+        for (int r = 0; r < 4; ++r) {
+            const f32x2 a = pack2(v[i][r].x, v[i][r].y), b = pack2(v[i][r].z, v[i][r].w);
+            w[r] = usual ? (uint32_t)q8_pair(fast(a)) | (uint32_t)q8_pair(fast(b)) << 16 : (uint32_t)q8_pair(plain(a)) | (uint32_t)q8_pair(plain(b)) << 16;
+            if (qt && 4 * k4 + r < kn && 4 * lane < nn) put_bytes(qt + (int64_t)(k0 + 4 * k4 + r) * ldqt + n0 + 4 * lane, w[r], nn - 4 * lane, words_t);
         }
+        const uint32_t a01 = __byte_perm(w[0], w[1], 0x5140), a23 = __byte_perm(w[2], w[3], 0x5140), b01 = __byte_perm(w[0], w[1], 0x7362), b23 = __byte_perm(w[2], w[3], 0x7362);
+        turned[4 * lane][k4] = __byte_perm(a01, a23, 0x5410);
+        turned[4 * lane + 1][k4] = __byte_perm(a01, a23, 0x7632);
+        turned[4 * lane + 2][k4] = __byte_perm(b01, b23, 0x5410);
+        turned[4 * lane + 3][k4] = __byte_perm(b01, b23, 0x7632);
+    }
+    if (!q) return;
+    __syncthreads();
+    for (int n = warp; n < nn; n += QW_THREADS / 32)
+        if (4 * lane < kn) put_bytes(q + (int64_t)(n0 + n) * ldq + k0 + 4 * lane, turned[n][lane], kn - 4 * lane, words);
 }
 
 // ---------------------------------------------------------------- host side
@@ -539,39 +714,92 @@ static bool vectors(const NormArgs& a, int size) {
     return on16(a.out, a.ld_out, out_size);
 }
 
-template <typename T, bool VEC, int W, int C> static cudaError_t norm_go(const NormArgs& a, cudaStream_t st) {
-    constexpr int ROWS = W == 1 ? NORM_WARPS : 1;
-    return launch_dependent(rms_norm_kernel<T, VEC, W, C>, dim3((unsigned)ceil_div(a.n, ROWS)), dim3(32 * (W == 1 ? NORM_WARPS : W)), 0, st, a);
-}
-// rows up to this many columns stay in a warp's registers; up to eight times that, in a block's
-constexpr int WARP_COLS = 2048;
+// A stream of rows to every warp: blocks of STREAM_WARPS warps, as many as an SM's shared memory takes (at most eight).  The rows
+// have to be enough to fill the streams.
+constexpr int64_t SMEM_PER_SM = 227 * 1024;
+static int stream_blocks(int smem) { const int64_t n = SMEM_PER_SM / (smem + 1024); return (int)(n < 8 ? n : 8); }
+static bool stream_fits(int64_t n, int blocks) { return n >= (int64_t)sm_count() * blocks * STREAM_WARPS * 2; }
 
+// f(C) with the smallest C that holds the row; false: none does
+template <typename T, typename Fn> static bool stream_width(int cols, Fn&& fn) {
+    const int pieces = (int)ceil_div((int64_t)cols * (int)sizeof(T), 512);
+    if (pieces <= 1) fn(std::integral_constant<int, 1>{});
+    else if (pieces <= 2) fn(std::integral_constant<int, 2>{});
+    else if (pieces <= 4) fn(std::integral_constant<int, 4>{});
+    else if (pieces <= 6) fn(std::integral_constant<int, 6>{});
+    else if (pieces <= 8) fn(std::integral_constant<int, 8>{});
+    else if (sizeof(T) == 4 && pieces <= 16) {             // (bf16: fewer values in twice the registers)
+        if constexpr (sizeof(T) == 4) { if (pieces <= 12) fn(std::integral_constant<int, 12>{}); else fn(std::integral_constant<int, 16>{}); }
+    } else return false;
+    return true;
+}
+// true: the rows go by streams, *e is the launch's result
+template <typename T, int C, bool RES> static bool back_stream_go(const NormArgs& a, int* grid, cudaError_t* e, cudaStream_t st) {
+    constexpr int SMEM = stream_smem(RES ? 3 : 2, C);
+    int blocks = stream_blocks(SMEM);
+    if (blocks > GEAR_NORM_WORKSPACE_ROWS / sm_count()) blocks = GEAR_NORM_WORKSPACE_ROWS / sm_count();
+    if (blocks < 1 || !stream_fits(a.n, blocks)) return false;
+    *grid = sm_count() * blocks;
+    *e = allow_smem<rms_norm_back_stream_kernel<T, C, RES>>(SMEM);
+    if (*e == cudaSuccess) *e = launch_dependent(rms_norm_back_stream_kernel<T, C, RES>, dim3((unsigned)*grid), dim3(32 * STREAM_WARPS), (size_t)SMEM, st, a);
+    return true;
+}
+template <typename T> static bool back_stream(const NormArgs& a, int* grid, cudaError_t* e, cudaStream_t st) {
+    bool went = false;
+    stream_width<T>(a.cols, [&](auto c) { went = a.dres ? back_stream_go<T, decltype(c)::value, true>(a, grid, e, st) : back_stream_go<T, decltype(c)::value, false>(a, grid, e, st); });
+    return went;
+}
+
+template <typename T, bool VEC, bool ONE, int C> static cudaError_t norm_go(const NormArgs& a, cudaStream_t st) {
+    const int warps = ONE ? NORM_ROWS : (int)ceil_div(ceil_div(a.cols, Chunk<T, VEC>::COLS), C);
+    return launch_dependent(rms_norm_kernel<T, VEC, ONE, C>, dim3((unsigned)(ONE ? ceil_div(a.n, NORM_ROWS) : a.n)), dim3(32 * warps), 0, st, a);
+}
 template <typename T, bool VEC> static cudaError_t norm_by_width(const NormArgs& a, cudaStream_t st) {
-    constexpr int COLS = Chunk<T, VEC>::COLS, C = WARP_COLS / COLS;
-    // few rows: all eight warps of a block on a row, which then waits for a fraction of the loads
-    const bool few = a.n < (int64_t)sm_count() * 8 && a.cols > COLS;
-    if (few && a.cols <= WARP_COLS) return norm_go<T, VEC, 8, (C + 7) / 8>(a, st);
-    if (a.cols <= WARP_COLS / 4) return norm_go<T, VEC, 1, C / 4>(a, st);
-    if (a.cols <= WARP_COLS) return norm_go<T, VEC, 1, C>(a, st);
-    if (a.cols <= 8 * WARP_COLS / 2) return norm_go<T, VEC, 8, C / 2>(a, st);
+    constexpr int COLS = Chunk<T, VEC>::COLS;
+    const int64_t pieces = ceil_div(a.cols, COLS);
+    // Few rows: as many warps to a row as there are pieces, each of which then waits for its own loads alone.  Many: a row to a warp, and
+    // what a warp does once is done once a row.  Wide rows in between: two pieces a warp.  e4m3 outputs, us, one piece / two pieces a warp / a
+    // row to a warp.  bf16, 1536 columns, residual: 600 rows 3.2 / 3.5 / 5.8; 2500: 7.1 / 6.6 / 7.0; 12000: 30.0 / 25.4 / 30.8; 40000: 90.9 / 72.3 /
+    // 74.9; 262144: 576 / 445 / 417.  fp32, 1536 columns by ID: 12000: - / 33.6 / 35.9; 40000: - / 102.9 / 94.6.  bf16, 500 columns: 600: 2.4 / 3.1 /
+    // 3.9; 2500: 4.8 / 4.3 / 4.4; 12000: 16.2 / 13.3 / 11.7; 40000: 51.4 / 40.9 / 35.1.
+    if (pieces == 1) return norm_go<T, VEC, true, 1>(a, st);
+    if (pieces > 4 && pieces <= 16 && a.n >= 1024 && a.n < 24576) return norm_go<T, VEC, false, 2>(a, st);
+    if (a.n >= 1024) {
+        if (pieces <= 2) return norm_go<T, VEC, true, 2>(a, st);
+        if (pieces <= 4) return norm_go<T, VEC, true, 4>(a, st);
+        if (pieces <= 6) return norm_go<T, VEC, true, 6>(a, st);
+        if (pieces <= 8) return norm_go<T, VEC, true, 8>(a, st);
+        if constexpr (COLS == 128) {
+            if (pieces <= 12) return norm_go<T, VEC, true, 12>(a, st);
+            if (pieces <= 16) return norm_go<T, VEC, true, 16>(a, st);
+        }
+    }
+    if (pieces <= 8) return norm_go<T, VEC, false, 1>(a, st);
+    if (pieces <= 16) return norm_go<T, VEC, false, 2>(a, st);
+    if (pieces <= 32) return norm_go<T, VEC, false, 4>(a, st);
+    if constexpr (COLS == 128) { if (pieces <= 64) return norm_go<T, VEC, false, 8>(a, st); }
     const int64_t blocks = a.n < (int64_t)sm_count() * 8 ? a.n : (int64_t)sm_count() * 8;
     return launch_dependent(rms_norm_wide_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, st, a);
 }
 
-template <typename T, bool VEC, int W, int C> static cudaError_t back_go(const NormArgs& a, int* blocks, cudaStream_t st) {
-    constexpr int ROWS = W == 1 ? NORM_WARPS : 1;
-    const int64_t want = ceil_div(a.n, ROWS);
-    *blocks = (int)(want < GEAR_NORM_WORKSPACE_ROWS ? want : GEAR_NORM_WORKSPACE_ROWS);
-    return launch_dependent(rms_norm_back_kernel<T, VEC, W, C>, dim3((unsigned)*blocks), dim3(32 * (W == 1 ? NORM_WARPS : W)),
-                            W == 1 ? (size_t)a.cols * 4 : 0, st, a);
+// PER_SM: blocks of 256 threads that an SM takes (in registers); the grid is no larger than what runs at once.
+template <typename T, bool VEC, int C, int R, int PER_SM> static cudaError_t back_go(const NormArgs& a, int* blocks, cudaStream_t st) {
+    const int64_t want = ceil_div(a.n, R), most = (int64_t)sm_count() * PER_SM;
+    *blocks = (int)(want < most ? want : most);
+    if (*blocks > GEAR_NORM_WORKSPACE_ROWS) *blocks = GEAR_NORM_WORKSPACE_ROWS;
+    const int warps = (int)ceil_div(ceil_div(a.cols, Chunk<T, VEC>::COLS), C);
+    return launch_dependent(rms_norm_back_kernel<T, VEC, C, R, PER_SM>, dim3((unsigned)*blocks), dim3(32 * warps), 0, st, a);
 }
 template <typename T, bool VEC> static cudaError_t back_by_width(const NormArgs& a, int* blocks, cudaStream_t st) {
-    constexpr int COLS = Chunk<T, VEC>::COLS, C = WARP_COLS / COLS;
-    const bool few = a.n < (int64_t)sm_count() * 8 && a.cols > COLS;
-    if (few && a.cols <= WARP_COLS) return back_go<T, VEC, 8, (C + 7) / 8>(a, blocks, st);
-    if (a.cols <= WARP_COLS / 4) return back_go<T, VEC, 1, C / 4>(a, blocks, st);
-    if (a.cols <= WARP_COLS) return back_go<T, VEC, 8, (C + 7) / 8>(a, blocks, st);
-    if (a.cols <= 8 * WARP_COLS / 2) return back_go<T, VEC, 8, C / 2>(a, blocks, st);
+    constexpr int COLS = Chunk<T, VEC>::COLS;
+    const int64_t pieces = ceil_div(a.cols, COLS);
+    cudaError_t e = cudaSuccess;
+    if constexpr (VEC) { if (back_stream<T>(a, blocks, &e, st)) return e; }
+    // one row at a time while there are not more rows than blocks
+    if (pieces <= 8) return a.n <= GEAR_NORM_WORKSPACE_ROWS ? back_go<T, VEC, 1, 1, 4>(a, blocks, st) : back_go<T, VEC, 1, 2, 4>(a, blocks, st);
+    if (pieces <= 16) return back_go<T, VEC, 2, 1, 3>(a, blocks, st);
+    if (pieces <= 32) return back_go<T, VEC, 4, 1, 2>(a, blocks, st);
+    if constexpr (COLS == 128) { if (pieces <= 64) return back_go<T, VEC, 8, 1, 1>(a, blocks, st); }
     *blocks = (int)(a.n < GEAR_NORM_WORKSPACE_ROWS ? a.n : GEAR_NORM_WORKSPACE_ROWS);
     return launch_dependent(rms_norm_back_wide_kernel<T>, dim3((unsigned)*blocks), dim3(256), 0, st, a);
 }
@@ -589,16 +817,15 @@ cudaError_t launch_rms_norm_backward(const NormArgs& a, int dtype, cudaStream_t 
     if (dtype == GEAR_BF16) e = vectors(a, 2) ? back_by_width<__nv_bfloat16, true>(a, &blocks, st) : back_by_width<__nv_bfloat16, false>(a, &blocks, st);
     else e = vectors(a, 4) ? back_by_width<float, true>(a, &blocks, st) : back_by_width<float, false>(a, &blocks, st);
     if (e != cudaSuccess || !a.dweight) return e;
-    return launch_dependent(norm_dweight_kernel, dim3((unsigned)ceil_div(a.cols, 32)), dim3(256), 0, st, static_cast<const float*>(a.parts), blocks,
+    return launch_dependent(norm_dweight_kernel, dim3((unsigned)ceil_div(a.cols, 32)), dim3(1024), 0, st, static_cast<const float*>(a.parts), blocks,
                             a.cols, a.dweight);
 }
 
 cudaError_t launch_q8_weights(const float* W, int64_t ldw, int K, int N, uint8_t* q, int64_t ldq, float* scale, uint8_t* qt, int64_t ldqt,
                               float* scale_t, cudaStream_t st) {
-    constexpr int SMEM = Q8_BLOCK * (Q8_BLOCK + 1) * 4;
-    if (const cudaError_t e = allow_smem<q8_weights_kernel>(SMEM)) return e;
-    return launch_dependent(q8_weights_kernel, dim3((unsigned)ceil_div(K, Q8_BLOCK), (unsigned)ceil_div(N, Q8_BLOCK)), dim3(256), (size_t)SMEM, st,
-                            W, ldw, K, N, q, ldq, scale, qt, ldqt, scale_t);
+    const int vec = on16(W, ldw, 4);
+    return launch_dependent(q8_weights_kernel, dim3((unsigned)ceil_div(K, Q8_BLOCK), (unsigned)ceil_div(N, Q8_BLOCK)), dim3(QW_THREADS), 0, st,
+                            W, ldw, vec, K, N, q, ldq, scale, qt, ldqt, scale_t);
 }
 
 }  // namespace gear
