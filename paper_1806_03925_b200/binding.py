@@ -412,6 +412,8 @@ def gear_adam_dense(param, grad, m, v, t: int, cfg: gear_adam, stream=None):
 # behind the other); all tensors of a call are on the current device.
 # ---------------------------------------------------------------------------
 _FLOATS = {torch.float32: GEAR_F32, torch.bfloat16: GEAR_BF16}
+_E4M3 = {torch.float8_e4m3fn: GEAR_E4M3, torch.uint8: GEAR_E4M3}
+_F32 = {torch.float32: GEAR_F32}
 _OUTS = {torch.float32: GEAR_F32, torch.bfloat16: GEAR_BF16, torch.float8_e4m3fn: GEAR_E4M3, torch.uint8: GEAR_E4M3}
 
 
@@ -419,68 +421,90 @@ def _refuse(what: str):
     raise TypeError("libgear: " + what)
 
 
+def _refuse_rows(t, dtypes, dev: int, n, cols):
+    if not torch.is_tensor(t) or t.get_device() != dev:
+        _refuse("takes device memory of the current device; got %s" % (t.device if torch.is_tensor(t) else type(t)))
+    if t.dtype not in dtypes:
+        _refuse("does not take %s here" % t.dtype)
+    if t.dim() == 2 and t.stride(1) != 1 and t.shape[1] > 1:
+        _refuse("takes rows whose values lie one behind the other")
+    _refuse("rows of shape %s; needed: %s x %s" % (tuple(t.shape), "any" if n is None else n, "any" if cols is None else cols))
+
+
+# (A call's checks are most of what it costs the host: these two look at a tensor as few times as they can.)
 def _rows(t: torch.Tensor, dtypes, dev: int, n: Optional[int] = None, cols: Optional[int] = None):
     """(pointer, distance between rows, type) of a 2-D tensor of rows, with at least n of them and exactly cols columns."""
-    if t.get_device() != dev:
-        _refuse("takes device memory of the current device; got a %s tensor" % t.device)
-    code = dtypes.get(t.dtype)
-    if code is None:
-        _refuse("does not take %s here" % t.dtype)
-    if t.dim() != 2 or (cols is not None and t.shape[1] != cols) or (n is not None and t.shape[0] < n):
-        _refuse("rows of shape %s; needed: %s x %s" % (tuple(t.shape), "any" if n is None else n, "any" if cols is None else cols))
-    ld, one = t.stride()
-    if one != 1 and t.shape[1] > 1:
-        _refuse("takes rows whose values lie one behind the other")
-    return t.data_ptr(), ld if t.shape[0] > 1 else max(ld, t.shape[1]), code
+    try:
+        code = dtypes[t.dtype]
+        have, wide = t.shape
+        ld, one = t.stride()
+    except (KeyError, ValueError, AttributeError):
+        _refuse_rows(t, dtypes, dev, n, cols)
+    if t.get_device() != dev or (one != 1 and wide > 1) or (n is not None and have < n) or (cols is not None and wide != cols):
+        _refuse_rows(t, dtypes, dev, n, cols)
+    return t.data_ptr(), (ld if have > 1 or ld > wide else wide), code
 
 
-def _vec(t: Optional[torch.Tensor], dtype, dev: int, n: Optional[int] = None):
+def _vec(t: Optional[torch.Tensor], dtype, dev: int, n: int = 0):
     """Pointer of a contiguous tensor of at least n values (None -> NULL)."""
     if t is None:
         return None
-    if t.get_device() != dev or t.dtype != dtype or not t.is_contiguous() or (n is not None and t.numel() < n):
-        _refuse("needs a contiguous %s tensor of the current device%s; got %s %s on %s" %
-                (dtype, "" if n is None else " with at least %d values" % n, tuple(t.shape), t.dtype, t.device))
+    if t.dtype is not dtype or t.get_device() != dev or t.numel() < n or not t.is_contiguous():
+        _refuse("needs a contiguous %s tensor of the current device with at least %d values; got %s %s on %s" %
+                (dtype, n, tuple(t.shape), t.dtype, t.device))
     return t.data_ptr()
 
 
-def _stream_here(stream: Optional[torch.cuda.Stream], dev: int) -> int:
-    if stream is None:
-        return torch._C._cuda_getCurrentRawStream(dev)
+_device = getattr(torch._C, "_cuda_getDevice", None)                    # (not there in a torch built without CUDA)
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream_here(stream: torch.cuda.Stream, dev: int) -> int:
     if stream.device_index != dev:
         _refuse("the stream is not one of the current device")
     return stream.cuda_stream
 
 
-def _row_count(n: Optional[int], t: torch.Tensor) -> int:
-    have = t.shape[0]
+def _row_count(n: Optional[int], t: torch.Tensor):
+    """(rows to compute, columns) of an output: n of them, or all."""
+    try:
+        have, cols = t.shape
+    except (ValueError, AttributeError):
+        _refuse("outputs are rows")
     if n is None:
-        return have
+        return have, cols
     if n < 0 or n > have:
         _refuse("n = %d outside [0, %d]" % (n, have))
-    return n
+    return n, cols
 
 
 def _blocks(cols: int) -> int:
-    return (cols + GEAR_Q8_BLOCK - 1) // GEAR_Q8_BLOCK
+    return (cols + 127) >> 7                         # of GEAR_Q8_BLOCK
 
 
 def gear_rms_norm(x, weight, out, scale=None, eps: float = 1e-6, res=None, res_out=None, ids=None, n: Optional[int] = None,
                   d_n=None, status=None, stream=None):
     """out[k] = RMS norm of x[k] (of x[ids[k]]) (+ res[k]) times weight, for k < n (default: all rows of out); out fp32, bf16 or, with
     scale, e4m3.  res_out[k] gets the sum."""
-    dev = torch._C._cuda_getDevice()
-    n = _row_count(n, out)
-    xp, ldx, code = _rows(x, _FLOATS, dev, None if ids is not None else n)
-    cols = x.shape[1]
-    same = {x.dtype: code}
-    rp, ldr, _ = (None, 0, 0) if res is None else _rows(res, same, dev, n, cols)
-    sp, lds, _ = (None, 0, 0) if res_out is None else _rows(res_out, same, dev, n, cols)
+    dev = _device()
+    n, cols = _row_count(n, out)
+    xp, ldx, code = _rows(x, _FLOATS, dev, None if ids is not None else n, cols)
     op, ldo, out_code = _rows(out, _OUTS, dev, n, cols)
+    rp = ldr = sp = lds = ip = vocab = None
+    if res is not None:
+        rp, ldr, same = _rows(res, _FLOATS, dev, n, cols)
+        if same != code:
+            _refuse("res has another type than x")
+    if res_out is not None:
+        sp, lds, same = _rows(res_out, _FLOATS, dev, n, cols)
+        if same != code:
+            _refuse("res_out has another type than x")
+    if ids is not None:
+        ip, vocab = _vec(ids, torch.int32, dev, n), x.shape[0]
     rc = (_lib or load()).gear_rms_norm(
-        xp, ldx, code, _vec(ids, torch.int32, dev, n), x.shape[0], rp, ldr, sp, lds, _vec(weight, torch.float32, dev, cols), n,
-        _vec(d_n, torch.int64, dev, 1), cols, eps, op, ldo, out_code, _vec(scale, torch.float32, dev, n * _blocks(cols)),
-        _vec(status, torch.int32, dev, 2), _stream_here(stream, dev))
+        xp, ldx, code, ip, vocab or 0, rp, ldr or 0, sp, lds or 0, _vec(weight, torch.float32, dev, cols), n, _vec(d_n, torch.int64, dev, 1),
+        cols, eps, op, ldo, out_code, _vec(scale, torch.float32, dev, n * _blocks(cols)), _vec(status, torch.int32, dev, 2),
+        _current_stream(dev) if stream is None else _stream_here(stream, dev))
     if rc != GEAR_OK:
         _check(rc, "gear_rms_norm")
 
@@ -489,53 +513,62 @@ def gear_rms_norm_backward(x, weight, dout, dx, dweight, workspace, eps: float =
                            d_n=None, status=None, stream=None):
     """Gradients of gear_rms_norm from x (the sum it normed) and dout: dx[k] (+ dres[k]) and dweight, either of which may be None;
     workspace: fp32 [GEAR_NORM_WORKSPACE_ROWS][cols], with dweight."""
-    dev = torch._C._cuda_getDevice()
-    n = _row_count(n, dout)
-    xp, ldx, code = _rows(x, _FLOATS, dev, None if ids is not None else n)
-    cols = x.shape[1]
-    same = {x.dtype: code}
-    gp, ldg, _ = _rows(dout, same, dev, n, cols)
-    rp, ldr, _ = (None, 0, 0) if dres is None else _rows(dres, same, dev, n, cols)
-    dp, ldd, _ = (None, 0, 0) if dx is None else _rows(dx, same, dev, n, cols)
-    if dweight is not None and workspace is None:
-        _refuse("dweight needs a workspace")
+    dev = _device()
+    n, cols = _row_count(n, dout)
+    xp, ldx, code = _rows(x, _FLOATS, dev, None if ids is not None else n, cols)
+    gp, ldg, same = _rows(dout, _FLOATS, dev, n, cols)
+    rp = dp = wp = ip = None
+    ldr = ldd = vocab = 0
+    if dres is not None:
+        rp, ldr, other = _rows(dres, _FLOATS, dev, n, cols)
+        same = same if other == code else -1
+    if dx is not None:
+        dp, ldd, other = _rows(dx, _FLOATS, dev, n, cols)
+        same = same if other == code else -1
+    if same != code:
+        _refuse("dout, dres and dx have the type of x")
+    if dweight is not None:
+        if workspace is None:
+            _refuse("dweight needs a workspace")
+        wp = _vec(workspace, torch.float32, dev, GEAR_NORM_WORKSPACE_ROWS * cols)
+    if ids is not None:
+        ip, vocab = _vec(ids, torch.int32, dev, n), x.shape[0]
     rc = (_lib or load()).gear_rms_norm_backward(
-        xp, ldx, code, _vec(ids, torch.int32, dev, n), x.shape[0], _vec(weight, torch.float32, dev, cols), gp, ldg, rp, ldr, n,
-        _vec(d_n, torch.int64, dev, 1), cols, eps, dp, ldd, _vec(dweight, torch.float32, dev, cols),
-        None if dweight is None else _vec(workspace, torch.float32, dev, GEAR_NORM_WORKSPACE_ROWS * cols),
-        _vec(status, torch.int32, dev, 2), _stream_here(stream, dev))
+        xp, ldx, code, ip, vocab, _vec(weight, torch.float32, dev, cols), gp, ldg, rp, ldr, n, _vec(d_n, torch.int64, dev, 1), cols, eps,
+        dp, ldd, _vec(dweight, torch.float32, dev, cols), wp, _vec(status, torch.int32, dev, 2),
+        _current_stream(dev) if stream is None else _stream_here(stream, dev))
     if rc != GEAR_OK:
         _check(rc, "gear_rms_norm_backward")
 
 
-_E4M3 = {torch.float8_e4m3fn: GEAR_E4M3, torch.uint8: GEAR_E4M3}
 
 
 def gear_q8_rows(x, q, scale, n: Optional[int] = None, d_n=None, stream=None):
     """q[k], scale[k] = x[k] in e4m3, one scale for every 128 columns."""
-    dev = torch._C._cuda_getDevice()
-    n = _row_count(n, q)
-    xp, ldx, code = _rows(x, _FLOATS, dev, n)
-    cols = x.shape[1]
+    dev = _device()
+    n, cols = _row_count(n, q)
+    xp, ldx, code = _rows(x, _FLOATS, dev, n, cols)
     qp, ldq, _ = _rows(q, _E4M3, dev, n, cols)
     if scale is None:
         _refuse("scale is needed")
     rc = (_lib or load()).gear_q8_rows(xp, ldx, code, n, _vec(d_n, torch.int64, dev, 1), cols, qp, ldq,
-                                       _vec(scale, torch.float32, dev, n * _blocks(cols)), _stream_here(stream, dev))
+                                       _vec(scale, torch.float32, dev, n * _blocks(cols)),
+                                       _current_stream(dev) if stream is None else _stream_here(stream, dev))
     if rc != GEAR_OK:
         _check(rc, "gear_q8_rows")
 
 
 def gear_q8_weights(W, q=None, scale=None, q_t=None, scale_t=None, stream=None):
     """W [K][N] fp32 in e4m3 as gear_q8_matmul reads it: q [N][K] and its scales, and / or q_t [K][N] and its scales."""
-    dev = torch._C._cuda_getDevice()
-    wp, ldw, _ = _rows(W, {torch.float32: GEAR_F32}, dev)
+    dev = _device()
+    wp, ldw, _ = _rows(W, _F32, dev)
     K, N = W.shape
     qp, ldq, _ = (None, 0, 0) if q is None else _rows(q, _E4M3, dev, N, K)
     tp, ldt, _ = (None, 0, 0) if q_t is None else _rows(q_t, _E4M3, dev, K, N)
     blocks = _blocks(K) * _blocks(N)
     rc = (_lib or load()).gear_q8_weights(wp, ldw, K, N, qp, ldq, _vec(scale, torch.float32, dev, blocks), tp, ldt,
-                                          _vec(scale_t, torch.float32, dev, blocks), _stream_here(stream, dev))
+                                          _vec(scale_t, torch.float32, dev, blocks),
+                                          _current_stream(dev) if stream is None else _stream_here(stream, dev))
     if rc != GEAR_OK:
         _check(rc, "gear_q8_weights")
 
@@ -543,22 +576,25 @@ def gear_q8_weights(W, q=None, scale=None, q_t=None, scale_t=None, stream=None):
 def gear_q8_matmul(a, a_scale, b, b_scale, out, status, n: Optional[int] = None, d_n=None, stream=None):
     """out[m] = a[m] . b^T with the scales of both, m < n (default: all rows of out); a [n][K], b [N][K] e4m3, rows at multiples of
     16 bytes; out fp32 or bf16 [n][N]; status: int32 [2], zero before the first call."""
-    dev = torch._C._cuda_getDevice()
-    n = _row_count(n, out)
-    ap, lda, _ = _rows(a, _E4M3, dev, n)
-    K = a.shape[1]
-    bp, ldb, _ = _rows(b, _E4M3, dev, None, K)
-    N = b.shape[0]
+    dev = _device()
+    n, N = _row_count(n, out)
     op, ldo, code = _rows(out, _FLOATS, dev, n, N)
+    ap, lda, _ = _rows(a, _E4M3, dev, n)
+    bp, ldb, _ = _rows(b, _E4M3, dev, N)
+    K = a.shape[1]
+    if b.shape != (N, K):
+        _refuse("b has the shape %s; needed: %d x %d" % (tuple(b.shape), N, K))
     if n == 1:                                       # (a single row's distance to the next one does not matter)
         lda = (lda + 15) & ~15
     if N == 1:
         ldb = (ldb + 15) & ~15
     if a_scale is None or b_scale is None:
         _refuse("both scales are needed")
-    rc = (_lib or load()).gear_q8_matmul(ap, lda, _vec(a_scale, torch.float32, dev, n * _blocks(K)), bp, ldb,
-                                         _vec(b_scale, torch.float32, dev, _blocks(N) * _blocks(K)), n, _vec(d_n, torch.int64, dev, 1), N, K,
-                                         op, ldo, code, _vec(status, torch.int32, dev, 2), _stream_here(stream, dev))
+    blocks = _blocks(K)
+    rc = (_lib or load()).gear_q8_matmul(ap, lda, _vec(a_scale, torch.float32, dev, n * blocks), bp, ldb,
+                                         _vec(b_scale, torch.float32, dev, _blocks(N) * blocks), n, _vec(d_n, torch.int64, dev, 1), N, K,
+                                         op, ldo, code, _vec(status, torch.int32, dev, 2),
+                                         _current_stream(dev) if stream is None else _stream_here(stream, dev))
     if rc != GEAR_OK:
         _check(rc, "gear_q8_matmul")
 
@@ -575,7 +611,7 @@ def make_grads(grads: Sequence[torch.Tensor], outs: Optional[Sequence[torch.Tens
     if len(where) != len(grads):
         _refuse("as many outs as grads")
     l = GradList()
-    l.device = torch._C._cuda_getDevice()
+    l.device = _device()
     l.items, l.count, l.tensors = (gear_grad * max(1, len(grads)))(), len(grads), (list(grads), list(where))
     written = set()
     for i, (g, o) in enumerate(zip(grads, where)):
@@ -597,18 +633,19 @@ def _grads(grads, outs=None) -> GradList:
     l = grads if isinstance(grads, GradList) else make_grads(grads, outs)
     if l is grads and outs is not None:
         _refuse("a list made with make_grads has its outs already")
-    if l.device != torch._C._cuda_getDevice():
+    if l.device != _device():
         _refuse("the gradients are not on the current device")
     return l
 
 
 def gear_grad_norm(grads, norm, workspace, stream=None):
     """norm[0] = the 2-norm of all gradients together (a list of tensors, or what make_grads returned)."""
-    dev = torch._C._cuda_getDevice()
+    dev = _device()
     if not isinstance(grads, GradList):
         grads = make_grads(grads, grads)
     l = _grads(grads)
-    rc = (_lib or load()).gear_grad_norm(l.items, l.count, _vec(norm, torch.float32, dev, 1), _clip_workspace(workspace, dev), _stream_here(stream, dev))
+    rc = (_lib or load()).gear_grad_norm(l.items, l.count, _vec(norm, torch.float32, dev, 1), _clip_workspace(workspace, dev),
+                                         _current_stream(dev) if stream is None else _stream_here(stream, dev))
     if rc != GEAR_OK:
         _check(rc, "gear_grad_norm")
 
@@ -616,10 +653,10 @@ def gear_grad_norm(grads, norm, workspace, stream=None):
 def gear_clip_grads(grads, max_norm: float, norm, workspace, outs=None, stream=None):
     """out_i = c g_i with c = min(1, max_norm / (norm + 1e-6)); norm (fp32 [2]) gets the norm and c.  grads: a list of tensors (clipped in
     place, or into outs), or what make_grads returned."""
-    dev = torch._C._cuda_getDevice()
+    dev = _device()
     l = _grads(grads, outs)
     rc = (_lib or load()).gear_clip_grads(l.items, l.count, max_norm, _vec(norm, torch.float32, dev, 2), _clip_workspace(workspace, dev),
-                                          _stream_here(stream, dev))
+                                          _current_stream(dev) if stream is None else _stream_here(stream, dev))
     if rc != GEAR_OK:
         _check(rc, "gear_clip_grads")
 

@@ -11,7 +11,7 @@
 namespace gear {
 
 constexpr int CLIP_THREADS = 256;
-constexpr int CLIP_BLOCKS = 592;           // four for every SM of a B200: also the shares in the workspace
+constexpr int CLIP_BLOCKS = 1184;          // eight for every SM of a B200 (94 million values in 150 tensors: 166 us; four: 171): also the shares in the workspace
 constexpr int CLIP_SMALL = 32, CLIP_LARGE = 1024;      // tensors a launch can take, as kernel parameters
 static_assert(CLIP_BLOCKS * sizeof(double) <= GEAR_CLIP_WORKSPACE_BYTES, "workspace");
 

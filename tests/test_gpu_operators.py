@@ -391,7 +391,7 @@ def workspace(gb):
 
 def clip_check(grads, outs, norm, max_norm):
     total = math.sqrt(sum(float((g.double() ** 2).sum()) for g in grads)) if grads else 0.0
-    c = min(1.0, max_norm / (total + 1e-6))
+    c = min(1.0, float(torch.tensor(max_norm, dtype=F32)) / (total + 1e-6))      # (max_norm is an fp32 argument)
     # 64-bit sums of exact squares; norm and c are rounded to fp32 once
     assert abs(float(norm[0]) - total) <= total * (U32 + 1e-12)
     assert abs(float(norm[1]) - c) <= c * (U32 + 1e-12)

@@ -99,4 +99,4 @@ def test_row_checks_of_the_binding(gb):
                 lambda: gb._vec(x, torch.int32, -1), lambda: gb._vec(x, torch.float32, 0), lambda: gb._row_count(7, x), lambda: gb._row_count(-1, x)):
         with pytest.raises(TypeError):
             bad()
-    assert gb._vec(None, torch.float32, 0) is None and gb._row_count(None, x) == 6 and gb._row_count(2, x) == 2
+    assert gb._vec(None, torch.float32, 0) is None and gb._row_count(None, x) == (6, 40) and gb._row_count(2, x) == (2, 40)
