@@ -12,11 +12,12 @@ namespace gear {
 
 constexpr int CLIP_THREADS = 256;
 constexpr int CLIP_BLOCKS = 1184;          // eight for every SM of a B200 (94 million values in 150 tensors: 166 us; four: 171): also the shares in the workspace
-constexpr int CLIP_SMALL = 32, CLIP_LARGE = 1024;      // tensors a launch can take, as kernel parameters
+constexpr int CLIP_SMALL = 32, CLIP_MIDDLE = 256, CLIP_LARGE = 1024;      // tensors a launch can take, as kernel parameters (30 KB of them cost the host 5 us)
+constexpr uint32_t CLIP_BACK = 8;          // tiles of a step backwards
 static_assert(CLIP_BLOCKS * sizeof(double) <= GEAR_CLIP_WORKSPACE_BYTES, "workspace");
 
-// A tensor's values in vectors of 16 bytes, `head` single values in front of the first.  A tile is `tile` vectors; the single
-// values at both ends belong to the tensor's first tile.
+// A tensor's values in vectors of 16 bytes, `head` single values in front of the first.  A tile is `tile` vectors; a
+// block goes through neighbouring tiles of a tensor as one stretch.  The single values at both ends belong to the tensor's first tile.
 template <int MAX> struct ClipList {
     const void* g[MAX];
     void* out[MAX];
@@ -83,11 +84,11 @@ template <bool BF16, typename Fn> __device__ __forceinline__ void clip_ends(int6
     if (behind + threadIdx.x < n) fn(behind + threadIdx.x);      // fewer than N
 }
 
-template <bool BF16> __device__ __forceinline__ double clip_sum_tile(const void* g, int64_t n, int head, int64_t v0, int tile) {
+template <bool BF16> __device__ __forceinline__ double clip_sum_stretch(const void* g, int64_t n, int head, int64_t v0, int64_t vectors) {
     typedef ClipVec<BF16> V;
     const typename V::T* p = static_cast<const typename V::T*>(g);
     const uint4* vec = reinterpret_cast<const uint4*>(p + head);
-    const int64_t v1 = min(v0 + (int64_t)tile, (n - head) / V::N);
+    const int64_t v1 = min(v0 + vectors, (n - head) / V::N);
     double sum = 0.0;
     int64_t v = v0 + threadIdx.x;
     auto add = [&](const uint4& q) {
@@ -108,13 +109,13 @@ template <bool BF16> __device__ __forceinline__ double clip_sum_tile(const void*
     return sum;
 }
 
-template <bool BF16> __device__ __forceinline__ void clip_scale_tile(const void* g, void* out, int64_t n, int head, int64_t v0, int tile, float c) {
+template <bool BF16> __device__ __forceinline__ void clip_scale_stretch(const void* g, void* out, int64_t n, int head, int64_t v0, int64_t vectors, float c) {
     typedef ClipVec<BF16> V;
     typedef typename V::T T;
     const T* p = static_cast<const T*>(g);
     T* o = static_cast<T*>(out);
     const uint4* vec = reinterpret_cast<const uint4*>(p + head);
-    const int64_t v1 = min(v0 + (int64_t)tile, (n - head) / V::N);
+    const int64_t v1 = min(v0 + vectors, (n - head) / V::N);
     const bool whole = (reinterpret_cast<uintptr_t>(o + head) & 15u) == 0;
     auto put = [&](int64_t v, const uint4& q) {
         const uint4 r = V::scaled(q, c);
@@ -163,10 +164,10 @@ clip_sum_kernel(const __grid_constant__ ClipList<MAX> l, double* __restrict__ sh
     double sum = 0.0;
     if (t < t1) {
         int i = clip_tensor_of(l, t);
-        for (; t < t1; ++t) {
-            while (t >= l.first[i + 1]) ++i;
-            const int64_t v0 = (int64_t)(t - l.first[i]) * l.tile;
-            sum += l.bf16[i] ? clip_sum_tile<true>(l.g[i], l.n[i], l.head[i], v0, l.tile) : clip_sum_tile<false>(l.g[i], l.n[i], l.head[i], v0, l.tile);
+        for (uint32_t end; t < t1; t = end, ++i) {
+            end = min(t1, l.first[i + 1]);
+            const int64_t v0 = (int64_t)(t - l.first[i]) * l.tile, vectors = (int64_t)(end - t) * l.tile;
+            sum += l.bf16[i] ? clip_sum_stretch<true>(l.g[i], l.n[i], l.head[i], v0, vectors) : clip_sum_stretch<false>(l.g[i], l.n[i], l.head[i], v0, vectors);
         }
     }
     sum = sum_over_block(sum, scratch);
@@ -200,12 +201,14 @@ clip_scale_kernel(const __grid_constant__ ClipList<MAX> l, const double* __restr
     clip_share(l.first[l.count], t0, t1);
     if (t0 >= t1) return;
     int i = clip_tensor_of(l, t1 - 1);
-    for (uint32_t t = t1; t-- > t0;) {
-        while (t < l.first[i]) --i;
+    for (uint32_t t = t1; t > t0;) {                       // backwards, a few tiles at a time
+        while (t <= l.first[i]) --i;
+        const uint32_t end = t;
+        t = max(max(t0, l.first[i]), end > CLIP_BACK ? end - CLIP_BACK : 0u);
         if (c == 1.f && l.out[i] == l.g[i]) continue;
-        const int64_t v0 = (int64_t)(t - l.first[i]) * l.tile;
-        if (l.bf16[i]) clip_scale_tile<true>(l.g[i], l.out[i], l.n[i], l.head[i], v0, l.tile, c);
-        else clip_scale_tile<false>(l.g[i], l.out[i], l.n[i], l.head[i], v0, l.tile, c);
+        const int64_t v0 = (int64_t)(t - l.first[i]) * l.tile, vectors = (int64_t)(end - t) * l.tile;
+        if (l.bf16[i]) clip_scale_stretch<true>(l.g[i], l.out[i], l.n[i], l.head[i], v0, vectors, c);
+        else clip_scale_stretch<false>(l.g[i], l.out[i], l.n[i], l.head[i], v0, vectors, c);
     }
 }
 
@@ -225,12 +228,11 @@ template <int MAX> static void clip_fill(ClipList<MAX>& l, const gear_grad* g, i
     }
 }
 
-// Tiles of 1024 vectors, or of as few as 256 while there are not enough for all blocks; so long that no launch counts past 2^31 of them.
+// Tiles of a vector for every thread of a block; longer ones where a launch would count past 2^30 of them.
 static int clip_tile(const gear_grad* g, int32_t count) {
     int64_t vectors = 0;
     for (int32_t i = 0; i < count; ++i) vectors += ceil_div(g[i].n, g[i].dtype == GEAR_BF16 ? 8 : 4);
-    int64_t tile = 1024;
-    while (tile > 256 && vectors / tile < CLIP_BLOCKS) tile >>= 1;
+    int64_t tile = CLIP_THREADS;
     while (vectors / tile > (1 << 30)) tile <<= 1;
     return (int)tile;
 }
@@ -266,8 +268,9 @@ static cudaError_t clip_run(const gear_grad* g, int32_t count, bool clip, float 
 
 cudaError_t launch_clip(const gear_grad* g, int32_t count, bool clip, float max_norm, float* norm, void* workspace, cudaStream_t st) {
     double* share = static_cast<double*>(workspace);
-    return count <= CLIP_SMALL ? clip_run<CLIP_SMALL>(g, count, clip, max_norm, norm, share, st)
-                               : clip_run<CLIP_LARGE>(g, count, clip, max_norm, norm, share, st);
+    return count <= CLIP_SMALL    ? clip_run<CLIP_SMALL>(g, count, clip, max_norm, norm, share, st)
+           : count <= CLIP_MIDDLE ? clip_run<CLIP_MIDDLE>(g, count, clip, max_norm, norm, share, st)
+                                  : clip_run<CLIP_LARGE>(g, count, clip, max_norm, norm, share, st);
 }
 
 }  // namespace gear

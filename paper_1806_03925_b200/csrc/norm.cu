@@ -125,7 +125,7 @@ template <bool VEC, int H> __device__ __forceinline__ float put_q8_early(void* r
 // written by the definition.
 template <bool VEC, int H, typename Fn> __device__ __forceinline__ void put_q8_late(void* row, int col0, int lane, int left, float* scale, float largest, float r, Fn&& value) {
     constexpr int LANES = VEC && H == 4 ? 16 : 32;                    // lanes that share a block
-    float s = q8_over_448(largest) * r;
+    float s = q8_usual_scale(largest, r);
     if (!q8_usual(largest, r)) {
         f32x2 v[H];
         value(v);
@@ -673,7 +673,7 @@ q8_weights_kernel(const float* __restrict__ W, int64_t ldw, int vec, int K, int 
     const Q8Quotient fast(largest);
     const Q8Plain plain(largest, 1.f);
     if (threadIdx.x == 0) {
-        const float s = usual ? fast.s : plain.scale;
+        const float s = usual ? q8_usual_scale(largest, 1.f) : plain.scale;
         if (q) scale[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = s;
         if (qt) scale_t[(int64_t)blockIdx.x * gridDim.y + blockIdx.y] = s;
     }

@@ -40,8 +40,12 @@ __device__ __forceinline__ float q8_larger(float a, float b, float c) {
 // remainder), so that a value lands on the other side of the middle between two e4m3 values only where v or the block's largest
 // have been rounded there.  Where that does not hold (largest infinite, a NaN, below 2^-90, or r largest below 2^-100: q8_usual) the
 // block is written by the definition (Q8Plain).
-__device__ __forceinline__ bool q8_usual(float largest) { return largest >= 0x1p-90f && largest <= FLT_MAX; }
-__device__ __forceinline__ bool q8_usual(float largest, float r) { return q8_usual(largest) && largest * r >= 0x1p-100f && largest * r <= FLT_MAX; }
+// (Blocks of zeros are usual too: zeros, and the smallest scale.)
+__device__ __forceinline__ bool q8_usual(float largest) { return (largest >= 0x1p-90f && largest <= FLT_MAX) || largest == 0.f; }
+__device__ __forceinline__ bool q8_usual(float largest, float r) {
+    const float h = largest * r;                 // (a NaN for zeros where r is infinite or NaN)
+    return q8_usual(largest) && h <= FLT_MAX && (h >= 0x1p-100f || largest == 0.f);
+}
 __device__ __forceinline__ float q8_over_448(float v) {
     constexpr float C = 1.0f / 448.0f;
     const float s = v * C;
@@ -52,12 +56,14 @@ struct Q8Quotient {
     __device__ __forceinline__ explicit Q8Quotient(float largest) {
         s = q8_over_448(largest);
         asm("rcp.approx.f32 %0, %1;" : "=f"(inv) : "f"(s));
+        if (largest == 0.f) inv = 0.f;
     }
     __device__ __forceinline__ f32x2 operator()(f32x2 v) const {
         const f32x2 q = mul2(v, both(inv));
         return fma2(fma2(q, both(-s), v), both(inv), q);
     }
 };
+__device__ __forceinline__ float q8_usual_scale(float largest, float r) { return largest == 0.f ? 0x1p-100f / 448.0f : q8_over_448(largest) * r; }
 struct Q8Plain {
     float scale, r;
     __device__ __forceinline__ Q8Plain(float largest, float factor) : r(factor) {

@@ -8,7 +8,7 @@
 // tensor cores fill the next accumulator.  A warp's columns lie in one block of weights and a lane holds one row, so a lane has one
 // factor per block of K; two columns are multiplied and added per instruction (fma.rn.f32x2).
 //
-// One persistent kernel, a CTA per SM: warp 0 streams the operands in by TMA (boxes of 128 bytes along K, which are one block),
+// One persistent kernel, a CTA per SM: warps 0 and 3 stream the operands in by TMA (boxes of 128 bytes along K, which are one block),
 // warps 1 and 2 issue the products (M 128, N BN, K 32: four per block), warps 4 to 11 add up and store.  Two warps share a quarter of the
 // tensor-memory lanes and split the columns.  Every wait is bounded: on a timeout the kernel says so in the status words, leaves
 // its loops, frees its tensor memory and returns.  No cluster launch and no multicast.
@@ -19,16 +19,20 @@
 namespace gear {
 
 constexpr int QP_EW = 8;                                     // epilogue warps
-constexpr int QP_THREADS = 128 + 32 * QP_EW;                 // a warpgroup of producer, issuers and one that idles; the epilogue's two
-constexpr int QP_OUT_BLOCK = 32 * 128;                       // a warp's results on their way out: 32 rows of 128 bytes, two of these a warp
+constexpr int QP_THREADS = 128 + 32 * QP_EW;                 // a warpgroup of producers and issuers; the epilogue's two
+constexpr int QP_OUT_BLOCK = 32 * 128;                       // a warp's results on their way out: 32 rows of 128 bytes
 
 template <int BN> struct QpCfg {
     static constexpr int A_BYTES = TC_BM * Q8_BLOCK, B_BYTES = BN * Q8_BLOCK, STAGE_BYTES = A_BYTES + B_BYTES;
-    static constexpr int STAGES = BN == 256 ? 3 : BN == 128 ? 5 : 6;
+    static constexpr int STAGES = BN == 256 ? 4 : 6;
+    static constexpr int OUT_BLOCKS = BN == 64 ? 2 : 1;      // a warp's blocks on their way out
     static constexpr int ACCS = BN == 256 ? 2 : 4;           // accumulators: all of the tensor memory, or half of it
     static constexpr int TMEM_COLS = BN * ACCS;
     static constexpr bool SPLIT = BN == 256;                 // registers are handed from the first warpgroup to the others
-    static constexpr int SMEM = STAGES * STAGE_BYTES + QP_EW * 2 * QP_OUT_BLOCK + 1024 /*alignment slack*/ + 256 /*barriers*/;
+    static constexpr int SMEM = STAGES * STAGE_BYTES + QP_EW * OUT_BLOCKS * QP_OUT_BLOCK + 1024 /*alignment slack*/ + 256 /*barriers*/;
+    // A barrier's phases are told apart by their parity, which takes one thread that waits for every one of them: a stage and an
+    // accumulator belong to the same producer and the same issuer (of the two that take blocks in turn) every time.
+    static_assert(STAGES % 2 == 0 && ACCS % 2 == 0, "stages and accumulators come round to the same producer and issuer");
     static_assert(SMEM <= 227 * 1024 && SMEM > 116 * 1024, "one CTA per SM: two would both ask for tensor memory");
 };
 
@@ -36,7 +40,7 @@ struct QpArgs {
     const float* a_scale; const float* b_scale;
     int64_t n; const int64_t* d_n;
     int N, K, n_tiles;
-    void* out; int64_t ld_out; int vec;                      // vec: rows of out start on 16-byte boundaries: map_out is set
+    void* out; int64_t ld_out; int unit;                     // rows of out start on boundaries of this many bytes: 16 (map_out is set), 4 or 2
     int32_t* status;
 };
 
@@ -57,33 +61,52 @@ __device__ __forceinline__ bool qp_warp_wait(uint32_t bar, uint32_t parity, int3
 __device__ __forceinline__ uint64_t pair64(uint32_t lo, uint32_t hi) { return (uint64_t)lo | (uint64_t)hi << 32; }
 __device__ __forceinline__ void fma_pair(uint64_t& acc, uint64_t v, uint64_t s) { asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc) : "l"(v), "l"(s)); }
 
-// A warp's 32 rows x 128 bytes from shared memory (16-byte pieces XOR-swizzled by the row) to the output: eight lanes per row.
-// out: the block's first row and column; rows, cols: how much of it there is to write.
+// A warp's 32 rows x 128 bytes from shared memory (16-byte pieces XOR-swizzled by the row) to the output, where the copy engine cannot
+// take them.  out: the block's first row and column; rows, cols: how much of it there is to write; unit: 16 where rows start on 16-byte
+// boundaries (eight lanes write a row), else 4 or 2: a row is written by all lanes, a word each, whole lines at a time (16 bytes a lane in
+// single values: 97839 x 400 x 306 in bf16 took 197 us).
 template <typename T>
-__device__ __forceinline__ void qp_store_block(uint32_t block, T* out, int64_t ld, int rows, int cols, bool vec, int lane) {
-    constexpr int PER = 16 / (int)sizeof(T);
-    const int piece = lane & 7, row0 = lane >> 3, col = piece * PER;
-    uint4 v[8];
+__device__ __forceinline__ void qp_store_block(uint32_t block, T* out, int64_t ld, int rows, int cols, int unit, int lane) {
+    constexpr int PER = 16 / (int)sizeof(T), IN_WORD = 4 / (int)sizeof(T);
+    if (unit == 16) {
+        const int piece = lane & 7, row0 = lane >> 3, col = piece * PER;
+        uint4 v[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int row = i * 4 + row0;
-        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v[i].x), "=r"(v[i].y), "=r"(v[i].z), "=r"(v[i].w)
-                     : "r"(block + (uint32_t)row * 128u + (((uint32_t)(piece ^ (row & 7))) << 4)) : "memory");
-    }
-    T* dst = out + row0 * ld + col;
-    if (vec && rows == 32 && col + PER <= cols) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4*>(dst + (int64_t)(4 * i) * ld) = v[i];
-    } else {
+        for (int i = 0; i < 8; ++i) {
+            const int row = i * 4 + row0;
+            asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v[i].x), "=r"(v[i].y), "=r"(v[i].z), "=r"(v[i].w)
+                         : "r"(block + (uint32_t)row * 128u + (((uint32_t)(piece ^ (row & 7))) << 4)) : "memory");
+        }
+        T* dst = out + row0 * ld + col;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             if (i * 4 + row0 >= rows) continue;
             T* d = dst + (int64_t)(4 * i) * ld;
-            if (vec && col + PER <= cols) *reinterpret_cast<uint4*>(d) = v[i];
+            if (col + PER <= cols) *reinterpret_cast<uint4*>(d) = v[i];
             else {
                 const T* e = reinterpret_cast<const T*>(&v[i]);
 #pragma unroll
                 for (int j = 0; j < PER; ++j) if (col + j < cols) d[j] = e[j];
+            }
+        }
+        return;
+    }
+    const int col = lane * IN_WORD;
+    for (int r0 = 0; r0 < rows; r0 += 8) {
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int row = r0 + i;
+            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[i]) : "r"(block + (uint32_t)row * 128u + (((uint32_t)((lane >> 2) ^ (row & 7))) << 4) + (uint32_t)(lane & 3) * 4u) : "memory");
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (r0 + i >= rows || col >= cols) continue;
+            T* d = out + (int64_t)(r0 + i) * ld + col;
+            if (sizeof(T) == 4 || (unit == 4 && col + 1 < cols)) *reinterpret_cast<uint32_t*>(d) = w[i];
+            else {
+                reinterpret_cast<uint16_t*>(d)[0] = (uint16_t)w[i];
+                if (col + 1 < cols) reinterpret_cast<uint16_t*>(d)[1] = (uint16_t)(w[i] >> 16);
             }
         }
     }
@@ -110,7 +133,7 @@ q8_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t tiles = (raw + 1023u) & ~1023u;
     const uint32_t out_blocks = tiles + STAGES * Cfg::STAGE_BYTES;
-    const uint32_t bars = out_blocks + QP_EW * 2 * QP_OUT_BLOCK;
+    const uint32_t bars = out_blocks + QP_EW * Cfg::OUT_BLOCKS * QP_OUT_BLOCK;
     auto full_bar = [&](int s) { return bars + 8u * s; };
     auto empty_bar = [&](int s) { return bars + 8u * (STAGES + s); };
     auto acc_full = [&](int a) { return bars + 8u * (2 * STAGES + a); };
@@ -145,26 +168,33 @@ q8_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
 
     if (warp < 4) {
         if (Cfg::SPLIT) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(QP_REGS_FEW));
-        // ---------------- TMA producer
-        if (warp == 0 && lane == 0) {
+        // ---------------- TMA producers: two warps, every second block of K each (one alone took 690 cycles from block to block); the
+        // whole warp walks the loop, so that what it counts stays in uniform registers, and one lane issues
+        if (warp == 0 || warp == 3) {
             Ring<STAGES> ring;
             uint32_t it = 0;
+            const uint32_t odd = (uint32_t)(warp == 3);
             bool ok = true;
             for (uint32_t t = blockIdx.x; t < total && ok; t += gridDim.x) {
                 const int mt = (int)(t / n_tiles), nt = (int)(t - (uint32_t)mt * n_tiles);      // the column tiles of a row tile side by side
                 for (int kb = 0; kb < kbs; ++kb, ++it, ring.next()) {
-                    if (!(ok = mbar_wait(empty_bar(ring.at), ring.round ^ 1u, err, 1))) break;
+                    if ((it & 1u) != odd) continue;
+                    ok = __all_sync(0xffffffffu, mbar_wait(empty_bar(ring.at), ring.round ^ 1u, err, 1));
+                    if (!ok) break;
                     const uint32_t a_dst = tiles + ring.at * Cfg::STAGE_BYTES, b_dst = a_dst + Cfg::A_BYTES, bar = full_bar(ring.at);
-                    mbar_expect_tx(bar, Cfg::STAGE_BYTES);
-                    tma_load_2d(a_dst, &map_a, bar, kb * Q8_BLOCK, mt * TC_BM);
-                    tma_load_2d(b_dst, &map_b, bar, kb * Q8_BLOCK, nt * BN);
+                    if (elect_one()) {
+                        mbar_expect_tx(bar, Cfg::STAGE_BYTES);
+                        tma_load_2d(a_dst, &map_a, bar, kb * Q8_BLOCK, mt * TC_BM);
+                        tma_load_2d(b_dst, &map_b, bar, kb * Q8_BLOCK, nt * BN);
+                    }
+                    __syncwarp();
                 }
             }
-            if (*reinterpret_cast<volatile int32_t*>(err) != 0) {
+            if (lane == 0 && *reinterpret_cast<volatile int32_t*>(err) != 0) {
                 // leaving early: let the copies already issued land before the CTA gives its shared memory back
                 const uint32_t first = it > (uint32_t)STAGES ? it - STAGES : 0u;
                 for (uint32_t j = first; j < it; ++j)
-                    for (uint32_t spin = 0; spin < (1u << 16) && !mbar_try(full_bar(j % STAGES), (j / STAGES) & 1u); ++spin)
+                    for (uint32_t spin = 0; (j & 1u) == odd && spin < (1u << 16) && !mbar_try(full_bar(j % STAGES), (j / STAGES) & 1u); ++spin)
                         __nanosleep(64);
             }
         }
@@ -200,7 +230,7 @@ q8_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         if (Cfg::SPLIT) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(QP_REGS_MANY));
         // ---------------- epilogue warps
         const int quarter = warp & 3, part = (warp - 4) >> 2;
-        const uint32_t block = out_blocks + (uint32_t)(warp - 4) * 2 * QP_OUT_BLOCK;
+        const uint32_t block = out_blocks + (uint32_t)(warp - 4) * Cfg::OUT_BLOCKS * QP_OUT_BLOCK;
         const uint32_t t_lane = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(part * COLS);
         // an accumulator is read in pieces of 32 columns, the next one on its way while one is added up: also across accumulators
         constexpr int WIDE = COLS >= 64 ? 32 : 16, PIECES = COLS / WIDE;
@@ -256,8 +286,8 @@ q8_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
 #pragma unroll
             for (int c = 0; c < (COLS + PIECE - 1) / PIECE; ++c) {
                 if (n0 + c * PIECE >= g.N) break;             // (uniform over the warp)
-                const uint32_t box = block + (uint32_t)(c & 1) * QP_OUT_BLOCK;
-                if (lane == 0) tma_store_wait_read<1>();      // the block's previous contents have been read (a copy is one group)
+                const uint32_t box = block + (uint32_t)(c % Cfg::OUT_BLOCKS) * QP_OUT_BLOCK;
+                if (lane == 0) tma_store_wait_read<Cfg::OUT_BLOCKS - 1>();      // the block's previous contents have been read (a copy is one group)
                 __syncwarp();
                 const uint32_t row = box + (uint32_t)lane * 128u;
 #pragma unroll
@@ -278,14 +308,14 @@ q8_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                     sts_u4(row + ((((uint32_t)j) ^ (uint32_t)(lane & 7)) << 4), make_uint4(w[0], w[1], w[2], w[3]));
                 }
                 const int rows = (int)min((int64_t)32, live - m0), cols = min(g.N, n0 + COLS) - (n0 + c * PIECE);     // (of half a piece: the other half is another warp's)
-                if (g.vec && COLS >= PIECE && rows > 0 && (rows == 32 || live == g.n)) {
+                if (g.unit == 16 && COLS >= PIECE && rows > 0 && (rows == 32 || live == g.n)) {
                     // the copy engine takes it from here and drops what lies past the edges
                     fence_async_smem();
                     __syncwarp();
                     if (lane == 0) tma_store_2d(&map_out, box, n0 + c * PIECE, (int)m0);
                 } else {
                     __syncwarp();
-                    if (rows > 0) qp_store_block<T>(box, out + m0 * g.ld_out + n0 + c * PIECE, g.ld_out, rows, cols, g.vec != 0, lane);
+                    if (rows > 0) qp_store_block<T>(box, out + m0 * g.ld_out + n0 + c * PIECE, g.ld_out, rows, cols, g.unit, lane);
                     __syncwarp();
                     if (lane == 0) asm volatile("cp.async.bulk.commit_group;" ::: "memory");      // (an empty group, in the place of a copy's)
                 }
@@ -388,9 +418,10 @@ template <int BN, typename T> static cudaError_t qp_go(const Q8Args& q, cudaStre
     g.a_scale = q.a_scale; g.b_scale = q.b_scale; g.n = q.n; g.d_n = q.d_n; g.N = q.N; g.K = q.K;
     g.n_tiles = (int)ceil_div(q.N, BN);
     g.out = q.out; g.ld_out = q.ld_out; g.status = q.status;
-    g.vec = (reinterpret_cast<uintptr_t>(q.out) & 15u) == 0 && (q.ld_out * (int64_t)sizeof(T)) % 16 == 0;
+    const uintptr_t starts = reinterpret_cast<uintptr_t>(q.out) | (uintptr_t)(q.ld_out * (int64_t)sizeof(T));
+    g.unit = starts % 16 == 0 ? 16 : starts % 4 == 0 ? 4 : 2;
     CUtensorMap mo = ma;
-    if (g.vec && !encode_map(&mo, TmaSpec{q.out, q.n, q.N, q.ld_out, 0, 1, 32, 128 / (int)sizeof(T), sizeof(T) == 4, 128})) return cudaErrorInvalidValue;
+    if (g.unit == 16 && !encode_map(&mo, TmaSpec{q.out, q.n, q.N, q.ld_out, 0, 1, 32, 128 / (int)sizeof(T), sizeof(T) == 4, 128})) return cudaErrorInvalidValue;
     const int64_t tiles = ceil_div(q.n, TC_BM) * g.n_tiles;
     if (tiles > INT32_MAX) return cudaErrorInvalidValue;     // (an output of 2^31 tiles fits no memory)
     const int grid = tiles < sm_count() ? (int)tiles : sm_count();
@@ -405,11 +436,13 @@ template <typename T> static cudaError_t qp_launch(const Q8Args& q, cudaStream_t
     if (q.n <= 2) return qf_go<2, T>(q, st);
     if (q.n <= 4) return qf_go<4, T>(q, st);
     if (q.n <= QF_ROWS) return qf_go<QF_ROWS, T>(q, st);
-    // the widest tiles that leave no SM without one
-    const int64_t m_tiles = ceil_div(q.n, TC_BM);
-    if (q.N <= 64 || m_tiles * ceil_div(q.N, 64) <= sm_count()) return qp_go<64, T>(q, st);
-    if (q.N <= 128 || m_tiles * ceil_div(q.N, 128) <= sm_count()) return qp_go<128, T>(q, st);
-    return qp_go<256, T>(q, st);
+    // The width of the tiles by what the busiest SM then has to do: its tiles, each some time per block of K and some for its start and its
+    // results (in 10 ns, from launches of 512 to 131072 rows, K 80 to 2048, N 64 to 1024).
+    const int64_t m_tiles = ceil_div(q.n, TC_BM), kbs = ceil_div(q.K, Q8_BLOCK);
+    auto cost = [&](int bn, int64_t block, int64_t rest) { return ceil_div(m_tiles * ceil_div(q.N, bn), sm_count()) * (kbs * block + rest); };
+    const int64_t c64 = cost(64, 36, 80), c128 = cost(128, 39, 100), c256 = cost(256, 55, 200);
+    if (c64 <= c128 && c64 <= c256) return qp_go<64, T>(q, st);
+    return c128 <= c256 ? qp_go<128, T>(q, st) : qp_go<256, T>(q, st);
 }
 
 cudaError_t launch_q8_product(const Q8Args& q, cudaStream_t st) {
