@@ -12,6 +12,8 @@
 // warps 1 and 2 issue the products (M 128, N BN, K 32: four per block), warps 4 to 11 add up and store.  Two warps share a quarter of the
 // tensor-memory lanes and split the columns.  Every wait is bounded: on a timeout the kernel says so in the status words, leaves
 // its loops, frees its tensor memory and returns.  No cluster launch and no multicast.
+#include <type_traits>
+
 #include "internal.h"
 #include "q8.cuh"
 #include "tc_ptx.cuh"
@@ -47,9 +49,6 @@ struct QpArgs {
 // Registers of a CTA with 128 columns a warp: launched with 168 a thread (384 x 168 = 64512), the epilogue's two warpgroups take 232,
 // the first one keeps 40 (256 x 232 + 128 x 40 = 64512).
 constexpr int QP_REGS_FEW = 40, QP_REGS_MANY = 232;
-
-__device__ __forceinline__ void qp_ld(uint32_t addr, uint32_t (&r)[32]) { tc_ld32(addr, r); }
-__device__ __forceinline__ void qp_ld(uint32_t addr, uint32_t (&r)[16]) { tc_ld16(addr, r); }
 
 // One lane waits for its warp.
 __device__ __forceinline__ bool qp_warp_wait(uint32_t bar, uint32_t parity, int32_t* err, int lane) {
@@ -233,8 +232,7 @@ q8_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         const uint32_t block = out_blocks + (uint32_t)(warp - 4) * Cfg::OUT_BLOCKS * QP_OUT_BLOCK;
         const uint32_t t_lane = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(part * COLS);
         // an accumulator is read in pieces of 32 columns, the next one on its way while one is added up: also across accumulators
-        constexpr int WIDE = COLS >= 64 ? 32 : 16, PIECES = COLS / WIDE;
-        static_assert(PIECES % 2 == 0, "the first piece is always in r[0]");
+        constexpr int WIDE = 32, PIECES = COLS / WIDE;
         Ring<ACCS> ring;
         bool ok = true;
         for (uint32_t t = blockIdx.x; t < total && ok; t += gridDim.x) {
@@ -247,37 +245,46 @@ q8_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             uint64_t acc[COLS / 2];
 #pragma unroll
             for (int i = 0; i < COLS / 2; ++i) acc[i] = 0ull;
-            float s_next = sa && sb ? __ldg(sa) * __ldg(sb) : 0.f;
+            // (the two factors are multiplied where they are used: a product right behind the loads would wait for them)
+            float sa_next = sa && sb ? __ldg(sa) : 0.f, sb_next = sa && sb ? __ldg(sb) : 0.f;
             uint32_t r[2][WIDE];
             ok = qp_warp_wait(acc_full(ring.at), ring.round, err, lane);
             tc_fence_after();
-            if (ok) qp_ld(t_lane + (uint32_t)(ring.at * BN), r[0]);
-            for (int kb = 0; kb < kbs && ok; ++kb) {
-                const uint32_t s32 = __float_as_uint(s_next);
+            if (ok) tc_ld32(t_lane + (uint32_t)(ring.at * BN), r[0]);
+            // one block of K, whose first piece is in (or on its way to) r[FIRST]; the next block's goes to r[(FIRST + PIECES) & 1]
+            auto block_of_k = [&](auto first, int kb) {
+                constexpr int FIRST = decltype(first)::value;
+                const uint32_t s32 = __float_as_uint(sa_next * sb_next);
                 const uint64_t s2 = pair64(s32, s32);
                 const bool more = kb + 1 < kbs;
-                if (more && sa && sb) s_next = __ldg(sa + kb + 1) * __ldg(sb + kb + 1);
+                if (more && sa && sb) { sa_next = __ldg(sa + kb + 1); sb_next = __ldg(sb + kb + 1); }
                 const int a = ring.at;
                 ring.next();
 #pragma unroll
                 for (int c = 0; c < PIECES; ++c) {
-                    tc_wait_ld(r[c & 1]);
-                    if (c + 1 < PIECES) qp_ld(t_lane + (uint32_t)(a * BN + (c + 1) * WIDE), r[(c + 1) & 1]);
+                    uint32_t (&now)[WIDE] = r[(FIRST + c) & 1];
+                    uint32_t (&then)[WIDE] = r[(FIRST + c + 1) & 1];
+                    tc_wait_ld(now);
+                    if (c + 1 < PIECES) tc_ld32(t_lane + (uint32_t)(a * BN + (c + 1) * WIDE), then);
                     else {
                         tc_fence_before();
                         __syncwarp();
-                        if (lane == 0) mbar_arrive_relaxed(acc_empty(a));      // all of it has been read (one arrival a warp: 256 took as long as the products)
+                        if (lane == 0) mbar_arrive_relaxed(acc_empty(a));      // all of it has been read
                         if (more) {
                             ok = qp_warp_wait(acc_full(ring.at), ring.round, err, lane);
                             tc_fence_after();
-                            qp_ld(t_lane + (uint32_t)(ring.at * BN), r[0]);
+                            tc_ld32(t_lane + (uint32_t)(ring.at * BN), then);
                         }
                     }
 #pragma unroll
-                    for (int i = 0; i < WIDE / 2; ++i) fma_pair(acc[c * (WIDE / 2) + i], pair64(r[c & 1][2 * i], r[c & 1][2 * i + 1]), s2);
+                    for (int i = 0; i < WIDE / 2; ++i) fma_pair(acc[c * (WIDE / 2) + i], pair64(now[2 * i], now[2 * i + 1]), s2);
                 }
+            };
+            for (int kb = 0; kb < kbs && ok; kb += 2) {
+                block_of_k(std::integral_constant<int, 0>{}, kb);
+                if (kb + 1 < kbs && ok) block_of_k(std::integral_constant<int, PIECES & 1>{}, kb + 1);
             }
-            tc_wait_ld(r[0]);                                 // (nothing is on its way, unless a wait gave up)
+            tc_wait_ld(r[0]); tc_wait_ld(r[1]);               // (nothing is on its way, unless a wait gave up)
             if (!ok) break;
             // a lane's row leaves in pieces of 128 bytes through the warp's block
             T* out = static_cast<T*>(g.out);
