@@ -97,7 +97,11 @@ template <bool VEC, int H> __device__ __forceinline__ float block_largest(const 
     float most = 0.f;
 #pragma unroll
     for (int e = 0; e < H; ++e) most = q8_larger(most, low(v[e]), high(v[e]));
-    if (VEC && H == 4) return __uint_as_float(__reduce_max_sync(lane < 16 ? 0xffffu : 0xffff0000u, __float_as_uint(most)));      // half a warp a block
+    if (VEC && H == 4) {                         // half a warp a block
+        const uint32_t m = __float_as_uint(most);
+        const uint32_t a = __reduce_max_sync(0xffffffffu, lane < 16 ? m : 0u), b = __reduce_max_sync(0xffffffffu, lane < 16 ? 0u : m);
+        return __uint_as_float(lane < 16 ? a : b);
+    }
     return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));
 }
 // A lane's values in e4m3 to a row; quotient: what becomes of a pair
@@ -121,21 +125,6 @@ template <bool VEC, int H> __device__ __forceinline__ float put_q8_early(void* r
     if (q8_usual(largest)) put_q8<VEC>(static_cast<uint8_t*>(row) + col0, lane, left, v, Q8Quotient(largest));
     return largest;
 }
-// The scales of the piece's blocks, once r is known (scale[0]: the first one's); value(v) gets the values again, where they have to be
-// written by the definition.
-template <bool VEC, int H, typename Fn> __device__ __forceinline__ void put_q8_late(void* row, int col0, int lane, int left, float* scale, float largest, float r, Fn&& value) {
-    constexpr int LANES = VEC && H == 4 ? 16 : 32;                    // lanes that share a block
-    float s = q8_usual_scale(largest, r);
-    if (!q8_usual(largest, r)) {
-        f32x2 v[H];
-        value(v);
-        const Q8Plain plain(largest, r);
-        put_q8<VEC>(static_cast<uint8_t*>(row) + col0, lane, left, v, plain);
-        s = plain.scale;
-    }
-    if (lane % LANES == 0 && (lane / LANES) * Q8_BLOCK < left) scale[lane / LANES] = s;
-}
-
 // A lane's values, times r, to a row of fp32 or bf16.
 template <bool VEC, int H> __device__ __forceinline__ void put_row(void* row, int col0, int lane, int left, int dtype, float r, f32x2 (&h)[H]) {
     const bool in = lane * 2 * H < left;                              // (VEC: all of the lane's values or none)
@@ -188,6 +177,45 @@ template <typename T> __device__ __forceinline__ void* row_of_out(const NormArgs
     return static_cast<char*>(a.out) + k * a.ld_out * (a.out_dtype == GEAR_E4M3 ? 1 : a.out_dtype == GEAR_BF16 ? 2 : 4);
 }
 
+// A piece of row k written by the definition, where its block is not a usual one: y is read again, from res_out if it has been kept there,
+// else made again.  (Out of line: divisions for every value in every piece of a row would be most of the kernel's instructions.)
+template <typename T, bool VEC>
+__device__ __noinline__ void q8_by_definition(const NormArgs& a, int64_t k, int col0, int lane, float largest, float r) {
+    typedef Chunk<T, VEC> Ch;
+    constexpr int H = Ch::E / 2;
+    const int left = a.cols - col0;
+    Ch y;
+    if (a.res_out) y.load(static_cast<const T*>(a.res_out) + k * a.ld_res_out + col0, lane, left);
+    else {
+        const T* x = row_of_x<T>(a, k, false);
+        if (x) y.load(x + col0, lane, left); else y.zero();
+        if (a.res) {
+            Ch s;
+            s.load(static_cast<const T*>(a.res) + k * a.ld_res + col0, lane, left);
+            y.add(s);
+        }
+    }
+    f32x2 v[H];
+    y.get(v);
+    if (a.weight) {
+        f32x2 w[H];
+        load_weight<VEC, H>(a.weight + col0, lane, left, w);
+#pragma unroll
+        for (int e = 0; e < H; ++e) v[e] = mul2(v[e], w[e]);
+    }
+    put_q8<VEC>(static_cast<uint8_t*>(row_of_out<T>(a, k)) + col0, lane, left, v, Q8Plain(largest, r));
+}
+// The scales of a piece's blocks, once r is known.
+template <typename T, bool VEC> __device__ __forceinline__ void put_q8_late(const NormArgs& a, int64_t k, float* scales, int col0, int lane, float largest, float r) {
+    constexpr int LANES = VEC && Chunk<T, VEC>::E == 8 ? 16 : 32;     // lanes that share a block
+    float s = q8_usual_scale(largest, r);
+    if (!q8_usual(largest, r)) {
+        q8_by_definition<T, VEC>(a, k, col0, lane, largest, r);
+        s = Q8Plain(largest, r).scale;
+    }
+    if (lane % LANES == 0 && col0 + (lane / LANES) * Q8_BLOCK < a.cols) scales[col0 / Q8_BLOCK + lane / LANES] = s;
+}
+
 // v summed over the warps that share a row; scratch: a word for each.  (All warps of the block call.)
 __device__ __forceinline__ float sum_over_row(float v, float* scratch, int part, int warps) {
     v = warp_sum(v);
@@ -203,7 +231,7 @@ constexpr int NORM_ROWS = 4;                     // rows per block where a warp 
 // A row to a warp (ONE) or to all warps of a block; C pieces of columns a warp: piece c * warps + part.
 template <typename T, bool VEC, bool ONE, int C>
 __global__ void __launch_bounds__(ONE ? 32 * NORM_ROWS : 256)
-rms_norm_kernel(const NormArgs a) {
+rms_norm_kernel(const __grid_constant__ NormArgs a) {
     typedef Chunk<T, VEC> Ch;
     constexpr int H = Ch::E / 2;
     __shared__ float scratch[8];
@@ -246,9 +274,11 @@ rms_norm_kernel(const NormArgs a) {
     for (int c = 0; c < C; ++c) {
         if (first(c) >= a.cols) continue;
         f32x2 v[H];
-        y[c].get(v);
+        if (a.normed) {
+            y[c].get(v);
 #pragma unroll
-        for (int e = 0; e < H; ++e) sum2 = fma2(v[e], v[e], sum2);
+            for (int e = 0; e < H; ++e) sum2 = fma2(v[e], v[e], sum2);
+        }
         if (q8) { value(c, v); largest[c] = put_q8_early<VEC, H>(out, first(c), lane, a.cols - first(c), v); }
     }
     float r = 1.f;
@@ -261,7 +291,7 @@ rms_norm_kernel(const NormArgs a) {
     for (int c = 0; c < C; ++c) {
         const int col0 = first(c);
         if (col0 >= a.cols) continue;
-        if (q8) put_q8_late<VEC, H>(out, col0, lane, a.cols - col0, a.scale + k * a.blocks + col0 / Q8_BLOCK, largest[c], r, [&](f32x2 (&v)[H]) { value(c, v); });
+        if (q8) put_q8_late<T, VEC>(a, k, a.scale + k * a.blocks, col0, lane, largest[c], r);
         else {
             f32x2 v[H];
             value(c, v);
@@ -273,7 +303,7 @@ rms_norm_kernel(const NormArgs a) {
 // Rows of any width: eight warps per row, three passes over it.
 template <typename T>
 __global__ void __launch_bounds__(256)
-rms_norm_wide_kernel(const NormArgs a) {
+rms_norm_wide_kernel(const __grid_constant__ NormArgs a) {
     typedef Chunk<T, false> Ch;
     __shared__ float scratch[8];
     wait_for_predecessor();
@@ -322,7 +352,7 @@ rms_norm_wide_kernel(const NormArgs a) {
             value(v);
             if (a.out_dtype == GEAR_E4M3) {
                 const float largest = put_q8_early<false, H>(out, col0, lane, a.cols - col0, v);
-                put_q8_late<false, H>(out, col0, lane, a.cols - col0, a.scale + k * a.blocks + col0 / Q8_BLOCK, largest, r, value);
+                put_q8_late<T, false>(a, k, a.scale + k * a.blocks, col0, lane, largest, r);
             } else put_row<false, H>(out, col0, lane, a.cols - col0, a.out_dtype, r, v);
         }
         __syncthreads();                         // scratch is free for the next row
