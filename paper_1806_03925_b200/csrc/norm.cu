@@ -360,88 +360,75 @@ rms_norm_wide_kernel(const __grid_constant__ NormArgs a) {
 }
 
 // ---------------------------------------------------------------- gradients
-// A block has R rows at a time, a lane the same C pieces of their columns in all of them: it keeps its weights and its part of dw in
-// registers for as long as it lives, and the rows' sums take one meeting of the block's warps for R rows.  At the end the block's part
-// of dw goes to its row of `parts`.  Nothing is added up in an order that could change.
-// (A row to each warp: 172 registers in bf16, 741 us for 131072 rows of 1536; a block to each row, 504.)
-template <typename T, bool VEC, int C, int R, int PER_SM>
+// A row to a block, a lane the same C pieces of columns of every row: it keeps its weights and its part of dw in registers for as long as
+// it lives.  The next row is on its way while the warps meet over one row's sums.  At the end the block's part of dw goes to its row
+// of `parts`.  Nothing is added up in an order that could change.
+template <typename T, bool VEC, int C, int PER_SM>
 __global__ void __launch_bounds__(256, PER_SM)
 rms_norm_back_kernel(const NormArgs a) {
     typedef Chunk<T, VEC> Ch;
-    __shared__ float scratch[2][8][2 * R];       // two sets in turn: a turn's sums are read by all before those of the turn after the next are written
+    constexpr int H = Ch::E / 2;
+    __shared__ float2 scratch[2][8];             // two sets in turn: a row's sums are read by all before those of the row after the next are written
     wait_for_predecessor();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     const int64_t live = live_rows(a);
     const float inv_cols = 1.0f / (float)a.cols;
-    f32x2 w[C][Ch::E / 2], dw[C][Ch::E / 2];
-    int left[C];                                 // columns from the piece's first one on
+    f32x2 w[C][H], dw[C][H];
+    auto first = [&](int c) { return (c * warps + warp) * Ch::COLS; };
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        const int col0 = (c * warps + warp) * Ch::COLS;
-        left[c] = a.cols - col0;
-        load_weight<VEC, Ch::E / 2>(a.weight && left[c] > 0 ? a.weight + col0 : nullptr, lane, left[c], w[c]);
+        load_weight<VEC, H>(a.weight && first(c) < a.cols ? a.weight + first(c) : nullptr, lane, a.cols - first(c), w[c]);
 #pragma unroll
-        for (int e = 0; e < Ch::E / 2; ++e) dw[c][e] = 0ull;
+        for (int e = 0; e < H; ++e) dw[c][e] = 0ull;
     }
+    Ch y[C], g[C], s[C];
+    auto fetch = [&](int64_t k) {
+        const T* x = row_of_x<T>(a, k, threadIdx.x == 0);
+        const T* dout = static_cast<const T*>(a.dout) + k * a.ld_dout;
+        const T* dres = a.dres ? static_cast<const T*>(a.dres) + k * a.ld_dres : nullptr;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            if (x) y[c].load(x + first(c), lane, a.cols - first(c)); else y[c].zero();
+            g[c].load(dout + first(c), lane, a.cols - first(c));
+            if (dres) s[c].load(dres + first(c), lane, a.cols - first(c)); else s[c].zero();
+        }
+    };
     int odd = 0;
-    for (int64_t k0 = (int64_t)blockIdx.x * R; k0 < live; k0 += (int64_t)gridDim.x * R, odd ^= 1) {
-        Ch y[R][C], g[R][C], s[R][C];
+    int64_t k = blockIdx.x;
+    if (k < live) fetch(k);
+    for (; k < live; k += gridDim.x, odd ^= 1) {
+        Ch y0[C], g0[C], s0[C];
+        f32x2 sq = 0ull, dot = 0ull;
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-            const int64_t k = k0 + i;
-            const T* x = k < live ? row_of_x<T>(a, k, threadIdx.x == 0) : nullptr;
-            const T* dout = k < live ? static_cast<const T*>(a.dout) + k * a.ld_dout : nullptr;
-            const T* dres = k < live && a.dres ? static_cast<const T*>(a.dres) + k * a.ld_dres : nullptr;
+        for (int c = 0; c < C; ++c) {
+            y0[c] = y[c]; g0[c] = g[c]; s0[c] = s[c];
+            f32x2 f[H], d[H];
+            y0[c].get(f); g0[c].get(d);
 #pragma unroll
-            for (int c = 0; c < C; ++c) {
-                const int col0 = (c * warps + warp) * Ch::COLS;
-                if (x) y[i][c].load(x + col0, lane, left[c]); else y[i][c].zero();
-                if (dout) g[i][c].load(dout + col0, lane, left[c]); else g[i][c].zero();
-                if (dres) s[i][c].load(dres + col0, lane, left[c]); else s[i][c].zero();
-            }
+            for (int e = 0; e < H; ++e) { sq = fma2(f[e], f[e], sq); dot = fma2(mul2(d[e], w[c][e]), f[e], dot); }
         }
-        float sum[2 * R];
-#pragma unroll
-        for (int i = 0; i < R; ++i) {
-            f32x2 sq = 0ull, dot = 0ull;
-#pragma unroll
-            for (int c = 0; c < C; ++c) {
-                f32x2 f[Ch::E / 2], d[Ch::E / 2];
-                y[i][c].get(f); g[i][c].get(d);
-#pragma unroll
-                for (int e = 0; e < Ch::E / 2; ++e) { sq = fma2(f[e], f[e], sq); dot = fma2(mul2(d[e], w[c][e]), f[e], dot); }
-            }
-            sum[2 * i] = warp_sum(low(sq) + high(sq)); sum[2 * i + 1] = warp_sum(low(dot) + high(dot));
-        }
+        if (k + gridDim.x < live) fetch(k + gridDim.x);
+        float2 sum = make_float2(warp_sum(low(sq) + high(sq)), warp_sum(low(dot) + high(dot)));
         if (warps > 1) {
-#pragma unroll
-            for (int i = 0; i < 2 * R; ++i) if (lane == i) scratch[odd][warp][i] = sum[i];
+            if (lane == 0) scratch[odd][warp] = sum;
             __syncthreads();
-#pragma unroll
-            for (int i = 0; i < 2 * R; ++i) sum[i] = 0.f;
-            for (int v = 0; v < warps; ++v)
-#pragma unroll
-                for (int i = 0; i < 2 * R; ++i) sum[i] += scratch[odd][v][i];
+            sum = make_float2(0.f, 0.f);
+            for (int v = 0; v < warps; ++v) { sum.x += scratch[odd][v].x; sum.y += scratch[odd][v].y; }
         }
+        const float r = 1.0f / sqrtf(sum.x * inv_cols + a.eps);
+        const float q = r * r * (sum.y * inv_cols);            // dx = r (g - y q): r alone may be large where y is small
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-            const int64_t k = k0 + i;
-            if (k >= live) continue;
-            const float r = 1.0f / sqrtf(sum[2 * i] * inv_cols + a.eps);
-            const float q = r * r * (sum[2 * i + 1] * inv_cols);          // dx = r (g - y q): r alone may be large where y is small
+        for (int c = 0; c < C; ++c) {
+            f32x2 f[H], d[H], o[H];
+            y0[c].get(f); g0[c].get(d); s0[c].get(o);
 #pragma unroll
-            for (int c = 0; c < C; ++c) {
-                f32x2 f[Ch::E / 2], d[Ch::E / 2], o[Ch::E / 2];
-                y[i][c].get(f); g[i][c].get(d); s[i][c].get(o);
-#pragma unroll
-                for (int e = 0; e < Ch::E / 2; ++e) {
-                    o[e] = fma2(both(r), fma2(f[e], both(-q), mul2(d[e], w[c][e])), o[e]);
-                    dw[c][e] = fma2(mul2(d[e], both(r)), f[e], dw[c][e]);
-                }
-                if (a.dx) {
-                    s[i][c].set(o);
-                    s[i][c].store(static_cast<T*>(a.dx) + k * a.ld_dx + (c * warps + warp) * Ch::COLS, lane, left[c]);
-                }
+            for (int e = 0; e < H; ++e) {
+                o[e] = fma2(both(r), fma2(f[e], both(-q), mul2(d[e], w[c][e])), o[e]);
+                dw[c][e] = fma2(mul2(d[e], both(r)), f[e], dw[c][e]);
+            }
+            if (a.dx) {
+                s0[c].set(o);
+                s0[c].store(static_cast<T*>(a.dx) + k * a.ld_dx + first(c), lane, a.cols - first(c));
             }
         }
     }
@@ -450,13 +437,11 @@ rms_norm_back_kernel(const NormArgs a) {
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
-        for (int e = 0; e < Ch::E; ++e) if (Ch::in(lane, e, left[c])) to[(c * warps + warp) * Ch::COLS + Ch::col(lane, e)] = half_of(dw[c][e / 2], e);
+        for (int e = 0; e < Ch::E; ++e) if (Ch::in(lane, e, a.cols - first(c))) to[first(c) + Ch::col(lane, e)] = half_of(dw[c][e / 2], e);
 }
 
-// A warp has rows of its own, one grid's warps apart, and STREAM - 1 of them on their way into shared memory while it works on one: a
-// lane copies (16 bytes at a time) the very pieces it will read, so that nobody waits for anybody.  A kernel that loads a row,
-// computes and stores keeps too little in flight: 262144 rows of 1536 in bf16 with a residual took 556 us with a row to a warp and 612
-// with a row to a block.
+// Narrow rows: a warp has rows of its own, one grid's warps apart, and the next one on its way into shared memory while it works on
+// one: a lane copies (16 bytes at a time) the very pieces it will read, so that nobody waits for anybody.
 constexpr int STREAM = 2, STREAM_WARPS = 4;
 constexpr int stream_smem(int arrays, int C) { return STREAM_WARPS * STREAM * arrays * C * 512; }
 
@@ -750,17 +735,14 @@ constexpr int64_t SMEM_PER_SM = 227 * 1024;
 static int stream_blocks(int smem) { const int64_t n = SMEM_PER_SM / (smem + 1024); return (int)(n < 8 ? n : 8); }
 static bool stream_fits(int64_t n, int blocks) { return n >= (int64_t)sm_count() * blocks * STREAM_WARPS * 2; }
 
-// f(C) with the smallest C that holds the row; false: none does
-template <typename T, typename Fn> static bool stream_width(int cols, Fn&& fn) {
+// f(C) with the smallest C that holds the row; false: none does, or the row is better off with a block (below)
+template <typename T, typename Fn> static bool stream_width(int cols, bool res, Fn&& fn) {
     const int pieces = (int)ceil_div((int64_t)cols * (int)sizeof(T), 512);
+    if (pieces > (res ? 4 : 6)) return false;
     if (pieces <= 1) fn(std::integral_constant<int, 1>{});
     else if (pieces <= 2) fn(std::integral_constant<int, 2>{});
     else if (pieces <= 4) fn(std::integral_constant<int, 4>{});
-    else if (pieces <= 6) fn(std::integral_constant<int, 6>{});
-    else if (pieces <= 8) fn(std::integral_constant<int, 8>{});
-    else if (sizeof(T) == 4 && pieces <= 16) {             // (bf16: fewer values in twice the registers)
-        if constexpr (sizeof(T) == 4) { if (pieces <= 12) fn(std::integral_constant<int, 12>{}); else fn(std::integral_constant<int, 16>{}); }
-    } else return false;
+    else fn(std::integral_constant<int, 6>{});
     return true;
 }
 // true: the rows go by streams, *e is the launch's result
@@ -776,7 +758,7 @@ template <typename T, int C, bool RES> static bool back_stream_go(const NormArgs
 }
 template <typename T> static bool back_stream(const NormArgs& a, int* grid, cudaError_t* e, cudaStream_t st) {
     bool went = false;
-    stream_width<T>(a.cols, [&](auto c) { went = a.dres ? back_stream_go<T, decltype(c)::value, true>(a, grid, e, st) : back_stream_go<T, decltype(c)::value, false>(a, grid, e, st); });
+    stream_width<T>(a.cols, a.dres != nullptr, [&](auto c) { went = a.dres ? back_stream_go<T, decltype(c)::value, true>(a, grid, e, st) : back_stream_go<T, decltype(c)::value, false>(a, grid, e, st); });
     return went;
 }
 
@@ -813,23 +795,26 @@ template <typename T, bool VEC> static cudaError_t norm_by_width(const NormArgs&
 }
 
 // PER_SM: blocks of 256 threads that an SM takes (in registers); the grid is no larger than what runs at once.
-template <typename T, bool VEC, int C, int R, int PER_SM> static cudaError_t back_go(const NormArgs& a, int* blocks, cudaStream_t st) {
-    const int64_t want = ceil_div(a.n, R), most = (int64_t)sm_count() * PER_SM;
-    *blocks = (int)(want < most ? want : most);
+template <typename T, bool VEC, int C, int PER_SM> static cudaError_t back_go(const NormArgs& a, int* blocks, cudaStream_t st) {
+    const int64_t most = (int64_t)sm_count() * PER_SM;
+    *blocks = (int)(a.n < most ? a.n : most);
     if (*blocks > GEAR_NORM_WORKSPACE_ROWS) *blocks = GEAR_NORM_WORKSPACE_ROWS;
     const int warps = (int)ceil_div(ceil_div(a.cols, Chunk<T, VEC>::COLS), C);
-    return launch_dependent(rms_norm_back_kernel<T, VEC, C, R, PER_SM>, dim3((unsigned)*blocks), dim3(32 * warps), 0, st, a);
+    return launch_dependent(rms_norm_back_kernel<T, VEC, C, PER_SM>, dim3((unsigned)*blocks), dim3(32 * warps), 0, st, a);
 }
 template <typename T, bool VEC> static cudaError_t back_by_width(const NormArgs& a, int* blocks, cudaStream_t st) {
     constexpr int COLS = Chunk<T, VEC>::COLS;
     const int64_t pieces = ceil_div(a.cols, COLS);
     cudaError_t e = cudaSuccess;
+    // Streams of narrow rows, a block to a wide one: in a block each warp has a piece or two, and the barrier's price is shared by few.  us, streams
+    // / blocks.  60000 rows of 128 in fp32 with the residual's gradient 27 / 77; 22069 of 368 in fp32 31 / 36; 131072 of 1536 in bf16 236 / 269, with
+    // the residual's gradient 327 / 295; 50000 of 2048 in bf16 with it 198 / 145; 50000 of 1000 in fp32 with it 211 / 127; 30000 of 1536 in fp32 with it
+    // 224 / 131.
     if constexpr (VEC) { if (back_stream<T>(a, blocks, &e, st)) return e; }
-    // one row at a time while there are not more rows than blocks
-    if (pieces <= 8) return a.n <= GEAR_NORM_WORKSPACE_ROWS ? back_go<T, VEC, 1, 1, 4>(a, blocks, st) : back_go<T, VEC, 1, 2, 4>(a, blocks, st);
-    if (pieces <= 16) return back_go<T, VEC, 2, 1, 3>(a, blocks, st);
-    if (pieces <= 32) return back_go<T, VEC, 4, 1, 2>(a, blocks, st);
-    if constexpr (COLS == 128) { if (pieces <= 64) return back_go<T, VEC, 8, 1, 1>(a, blocks, st); }
+    if (pieces <= 8) return back_go<T, VEC, 1, 4>(a, blocks, st);
+    if (pieces <= 16) return back_go<T, VEC, 2, 2>(a, blocks, st);
+    if (pieces <= 32) return back_go<T, VEC, 4, 1>(a, blocks, st);
+    if constexpr (COLS == 128) { if (pieces <= 64) return back_go<T, VEC, 8, 1>(a, blocks, st); }
     *blocks = (int)(a.n < GEAR_NORM_WORKSPACE_ROWS ? a.n : GEAR_NORM_WORKSPACE_ROWS);
     return launch_dependent(rms_norm_back_wide_kernel<T>, dim3((unsigned)*blocks), dim3(256), 0, st, a);
 }
