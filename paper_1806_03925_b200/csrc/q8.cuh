@@ -36,9 +36,9 @@ __device__ __forceinline__ float q8_larger(float a, float b, float c) {
 // The 8-bit form of the values r v of a block (r: the norm's factor of the row, or 1):
 //     scale = max(r largest, 2^-100) / 448,   q = r v / scale.
 // r cancels out of the quotient, so q is v / (largest / 448), for which nothing has to be known of r yet: values go out before the
-// row's sum of squares is there.  Both divisions are rounded as divisions are (the product with the reciprocal, corrected by its
-// remainder), so that a value lands on the other side of the middle between two e4m3 values only where v or the block's largest
-// have been rounded there.  Where that does not hold (largest infinite, a NaN, below 2^-90, or r largest below 2^-100: q8_usual) the
+// row's sum of squares is there.  The divisor is kept in two parts, and the quotient is rounded once, as a division is (the product with
+// the reciprocal, corrected by its remainder), so that a value lands on the other side of the middle between two e4m3 values only where
+// that rounding, or those of v and of the block's largest, have put it there.  Where that does not hold (largest infinite, a NaN, below 2^-90, or r largest below 2^-100: q8_usual) the
 // block is written by the definition (Q8Plain).
 // (Blocks of zeros are usual too: zeros, and the smallest scale.)
 __device__ __forceinline__ bool q8_usual(float largest) { return (largest >= 0x1p-90f && largest <= FLT_MAX) || largest == 0.f; }
@@ -52,15 +52,16 @@ __device__ __forceinline__ float q8_over_448(float v) {
     return fmaf(fmaf(s, -448.0f, v), C, s);
 }
 struct Q8Quotient {
-    float s, inv;
+    float s, rest, inv;                          // largest / 448 = s + rest
     __device__ __forceinline__ explicit Q8Quotient(float largest) {
         s = q8_over_448(largest);
+        rest = fmaf(s, -448.0f, largest) * (1.0f / 448.0f);
         asm("rcp.approx.f32 %0, %1;" : "=f"(inv) : "f"(s));
         if (largest == 0.f) inv = 0.f;
     }
     __device__ __forceinline__ f32x2 operator()(f32x2 v) const {
         const f32x2 q = mul2(v, both(inv));
-        return fma2(fma2(q, both(-s), v), both(inv), q);
+        return fma2(fma2(q, both(-rest), fma2(q, both(-s), v)), both(inv), q);
     }
 };
 __device__ __forceinline__ float q8_usual_scale(float largest, float r) { return largest == 0.f ? 0x1p-100f / 448.0f : q8_over_448(largest) * r; }
