@@ -206,6 +206,7 @@ q8_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             Ring<STAGES> ring;
             Ring<ACCS> acc;
             uint32_t mine = (uint32_t)warp & 1u;
+            uint32_t last_full = 0, last_empty = 0, full_round = 0, empty_round = 0;      // the barriers of the last block issued
             bool ok = true;
             for (uint32_t t = blockIdx.x; t < total && ok; t += gridDim.x) {
                 for (int kb = 0; kb < kbs; ++kb, ring.next(), acc.next(), mine ^= 1u) {
@@ -221,9 +222,14 @@ q8_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                         tc_commit(acc_full(acc.at));
                         tc_commit(empty_bar(ring.at));
                     }
+                    last_full = acc_full(acc.at); full_round = acc.round; last_empty = empty_bar(ring.at); empty_round = ring.round;
                     __syncwarp();
                 }
             }
+            // leaving early: what has been issued ends before the CTA gives its tensor memory and barriers back
+            if (!ok && last_full != 0)
+                for (uint32_t spin = 0; spin < (1u << 16) && !(mbar_try(last_full, full_round) && mbar_try(last_empty, empty_round)); ++spin)
+                    __nanosleep(64);
         }
     } else {
         if (Cfg::SPLIT) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(QP_REGS_MANY));

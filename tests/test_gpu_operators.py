@@ -384,7 +384,61 @@ def test_product_one_row_does_not_depend_on_its_neighbours(gb):
         check_product(many[:n], a[:n], sa[:n], b, sb)
 
 
+def test_products_side_by_side(gb):
+    """Products of several widths on two streams at once, each with a status of its own: the same bits as one after the other."""
+    data = [q8_data(n, K, N, n) for n, K, N in ((3000, 520, 64), (9000, 1040, 256), (700, 128, 1000), (20000, 260, 128))]
+    want = []
+    for a, sa, b, sb in data:
+        want.append(torch.empty((a.shape[0], b.shape[0]), device="cuda"))
+        gb.gear_q8_matmul(a, sa, b, sb, want[-1], status())
+    torch.cuda.synchronize()
+    streams, sts, outs = [torch.cuda.Stream() for _ in range(2)], [status(), status()], [[], []]
+    torch.cuda.synchronize()
+    for k, s in enumerate(streams):
+        with torch.cuda.stream(s):
+            for r in range(5):
+                for i, (a, sa, b, sb) in enumerate(data if k == 0 else data[::-1]):
+                    o = torch.empty((a.shape[0], b.shape[0]), device="cuda")
+                    gb.gear_q8_matmul(a, sa, b, sb, o, sts[k])
+                    outs[k].append((i if k == 0 else len(data) - 1 - i, o))
+    torch.cuda.synchronize()
+    assert sts[0].tolist() == sts[1].tolist() == [0, 0]
+    for i, o in outs[0] + outs[1]:
+        assert torch.equal(o, want[i])
+
+
+def test_product_says_that_a_wait_gave_up(gb):
+    """A status whose second word is not zero marks results as void until it is cleared; the call ends, and the next one is whole again."""
+    a, sa, b, sb = q8_data(5000, 520, 200, 5)
+    st, out = torch.tensor([0, 3], dtype=torch.int32, device="cuda"), torch.empty((5000, 200), device="cuda")
+    gb.gear_q8_matmul(a, sa, b, sb, out, st)
+    torch.cuda.synchronize()
+    assert st[0].item() & gb_timeout == gb_timeout and st[1].item() == 3
+    st.zero_()
+    gb.gear_q8_matmul(a, sa, b, sb, out, st)
+    assert st.tolist() == [0, 0]
+    check_product(out, a, sa, b, sb)
+
+
+def test_product_results_beyond_32_bits(gb):
+    n, K, N = (1 << 31) // 1024 + 300, 48, 1024
+    a, b = torch.zeros((n, K), dtype=torch.uint8, device="cuda").view(E4M3), e4m3_rows(N, K)
+    small, sa_small, b2, sb = q8_data(300, K, N, 7)
+    b.copy_(b2)
+    a[-300:] = small
+    sa = torch.ones((n, 1), device="cuda")
+    sa[-300:] = sa_small
+    st, out = status(), torch.full((n, N), 5.0, dtype=BF16, device="cuda")
+    gb.gear_q8_matmul(a, sa, b, sb, out, st)
+    assert st.tolist() == [0, 0]
+    check_product(out[-300:], a[-300:], sa[-300:], b, sb)
+    assert (out[:1000] == 0).all() and (out[n // 2:n // 2 + 1000] == 0).all()
+
+
 # ------------------------------------------------------------------------------------------------ clipping
+gb_timeout = 16                                     # GEAR_DEV_TIMEOUT
+
+
 def workspace(gb):
     return torch.full((gb.GEAR_CLIP_WORKSPACE_BYTES // 8,), float("nan"), dtype=torch.float64, device="cuda")
 
@@ -456,6 +510,17 @@ def test_clip_extremes(gb):
     g[7] = float("nan")
     gb.gear_clip_grads([g], 1.0, norm, ws)
     assert norm.isnan().all() and g.isnan().all()
+
+
+def test_clip_beyond_32_bits(gb):
+    n = (1 << 31) + 77
+    g = torch.full((n,), 0.5, dtype=BF16, device="cuda")
+    g[-1] = 3.0
+    norm, ws = torch.empty(2, device="cuda"), workspace(gb)
+    total = math.sqrt((n - 1) * 0.25 + 9.0)
+    gb.gear_clip_grads([g], total / 4, norm, ws)     # c = 1/4 but for roundings: 0.125 and 0.75 are bf16 values
+    assert abs(float(norm[0]) - total) <= total * (U32 + 1e-12)
+    assert (g[:1000] == 0.125).all() and (g[n // 2:n // 2 + 1000] == 0.125).all() and g[-1] == 0.75 and (g[-1000:-1] == 0.125).all()
 
 
 def test_clip_repeats(gb):
