@@ -445,10 +445,11 @@ template <int R, typename T> static cudaError_t qf_go(const Q8Args& q, cudaStrea
 }
 
 template <typename T> static cudaError_t qp_launch(const Q8Args& q, cudaStream_t st) {
-    if (q.n == 1) return qf_go<1, T>(q, st);
-    if (q.n <= 2) return qf_go<2, T>(q, st);
-    if (q.n <= 4) return qf_go<4, T>(q, st);
-    if (q.n <= QF_ROWS) return qf_go<QF_ROWS, T>(q, st);
+    // A warp for every column and R rows, while that makes few blocks for every SM: 1536 x 256, 16 rows 3.5 us (tiles 6.1), 32 rows 4.4 (6.3), 64
+    // rows 6.4 (6.4); 2048 x 1024, 8 rows 5.2 (7.0), 16 rows 7.8 (7.1).
+    const int rows = q.n <= 1 ? 1 : q.n <= 2 ? 2 : q.n <= 4 ? 4 : QF_ROWS;
+    if (ceil_div(q.N, 4) * ceil_div(q.n, rows) * rows <= 16 * (int64_t)sm_count())
+        return rows == 1 ? qf_go<1, T>(q, st) : rows == 2 ? qf_go<2, T>(q, st) : rows == 4 ? qf_go<4, T>(q, st) : qf_go<QF_ROWS, T>(q, st);
     // The width of the tiles by what the busiest SM then has to do: its tiles, each some time per block of K and some for its start and its
     // results (in 10 ns, from launches of 512 to 131072 rows, K 80 to 2048, N 64 to 1024).
     const int64_t m_tiles = ceil_div(q.n, TC_BM), kbs = ceil_div(q.K, Q8_BLOCK);

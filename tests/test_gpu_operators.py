@@ -317,7 +317,7 @@ def check_product(out, a, sa, b, sb):
 @pytest.mark.parametrize("out_dtype", [F32, BF16])
 @pytest.mark.parametrize("n,K,N", [(1, 1, 1), (1, 1536, 64), (2, 16, 8), (3, 100, 33), (4, 2048, 130), (7, 513, 65), (8, 128, 256), (9, 128, 64), (9, 1, 1), (100, 1000, 200),
                                    (128, 256, 64), (129, 129, 129), (130, 17, 300), (300, 640, 72), (1000, 48, 1000), (3001, 200, 1000), (5000, 384, 257),
-                                   (20000, 144, 520), (40000, 1040, 256)])
+                                   (20000, 144, 520), (40000, 1040, 256), (8, 300, 2000), (1, 200, 10000), (70, 77, 16), (1100, 500, 5)])
 def test_product(gb, n, K, N, out_dtype):
     a, sa, b, sb = q8_data(n, K, N, n + K + N)
     st, out = status(), torch.full((n, N), 5.0, dtype=out_dtype, device="cuda")
