@@ -251,17 +251,17 @@ static cudaError_t clip_run(const gear_grad* g, int32_t count, bool clip, float 
     do {
         last = at;
         clip_fill(l, g, count, &at, tile);
-        e = launch_dependent(clip_sum_kernel<MAX>, dim3(blocks), dim3(CLIP_THREADS), 0, st, l, share, (int)more);
+        e = launch_now(clip_sum_kernel<MAX>, dim3(blocks), dim3(CLIP_THREADS), 0, st, l, share, (int)more);
         more = true;
     } while (e == cudaSuccess && at < count);
     if (e != cudaSuccess) return e;
-    if (!clip) return launch_dependent(clip_norm_kernel, dim3(1), dim3(CLIP_THREADS), 0, st, static_cast<const double*>(share), blocks, norm);
+    if (!clip) return launch_now(clip_norm_kernel, dim3(1), dim3(CLIP_THREADS), 0, st, static_cast<const double*>(share), blocks, norm);
     // the tensors that were read last come first
     bool single = last == 0;
-    e = launch_dependent(clip_scale_kernel<MAX>, dim3(blocks), dim3(CLIP_THREADS), 0, st, l, static_cast<const double*>(share), blocks, max_norm, norm);
+    e = launch_now(clip_scale_kernel<MAX>, dim3(blocks), dim3(CLIP_THREADS), 0, st, l, static_cast<const double*>(share), blocks, max_norm, norm);
     for (at = 0; !single && at < last && e == cudaSuccess;) {
         clip_fill(l, g, last, &at, tile);
-        e = launch_dependent(clip_scale_kernel<MAX>, dim3(blocks), dim3(CLIP_THREADS), 0, st, l, static_cast<const double*>(share), blocks, max_norm, norm);
+        e = launch_now(clip_scale_kernel<MAX>, dim3(blocks), dim3(CLIP_THREADS), 0, st, l, static_cast<const double*>(share), blocks, max_norm, norm);
     }
     return e;
 }

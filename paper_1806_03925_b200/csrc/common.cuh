@@ -208,6 +208,19 @@ inline cudaError_t launch_dependent(void (*kernel)(KArgs...), dim3 grid, dim3 bl
     return launch_as(Op::DEPENDENT, kernel, grid, block, smem, st, std::forward<Args>(args)...);
 }
 
+// The same for the calls without a ctx, which nobody writes down: straight to the stream, the arguments from where they are (a list of
+// gradients is 30 KB of them).
+template <typename... KArgs, typename... Args>
+inline cudaError_t launch_now(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args&&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    launch_config(cfg, attr, Op::DEPENDENT, grid, block, smem, st);
+    return [&](const KArgs&... values) {
+        void* params[] = {const_cast<void*>(static_cast<const void*>(&values))...};
+        return cudaLaunchKernelExC(&cfg, reinterpret_cast<const void*>(kernel), params);
+    }(std::forward<Args>(args)...);
+}
+
 // Lets a kernel take `bytes` of dynamic shared memory beside its static one.  The attribute belongs to the kernel on one device: it is
 // asked for once on each, again where that failed.
 template <auto Kernel> inline cudaError_t allow_smem(int bytes) {

@@ -37,18 +37,21 @@ static int gather_args(const Op& o, OpList& l, void** params) {
     return (int)o.n_args;
 }
 
+void launch_config(cudaLaunchConfig_t& cfg, cudaLaunchAttribute (&attr)[1], Op::Attr kind, dim3 grid, dim3 block, size_t smem, cudaStream_t st) {
+    cfg.gridDim = grid; cfg.blockDim = block; cfg.dynamicSmemBytes = smem; cfg.stream = st;
+    if (kind == Op::PLAIN) return;
+    attr[0].id = kind == Op::DEPENDENT ? cudaLaunchAttributeProgrammaticStreamSerialization : cudaLaunchAttributeCooperative;
+    if (kind == Op::DEPENDENT) attr[0].val.programmaticStreamSerializationAllowed = 1;
+    else attr[0].val.cooperative = 1;
+    cfg.attrs = attr; cfg.numAttrs = 1;
+}
+
 cudaError_t launch_list_kernel(const Op& o, OpList& l, cudaStream_t st) {
     void* params[MAX_ARGS];
     if (gather_args(o, l, params) < 0) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = o.grid; cfg.blockDim = o.block; cfg.dynamicSmemBytes = o.bytes; cfg.stream = st;
     cudaLaunchAttribute attr[1];
-    if (o.attr != Op::PLAIN) {
-        attr[0].id = o.attr == Op::DEPENDENT ? cudaLaunchAttributeProgrammaticStreamSerialization : cudaLaunchAttributeCooperative;
-        if (o.attr == Op::DEPENDENT) attr[0].val.programmaticStreamSerializationAllowed = 1;
-        else attr[0].val.cooperative = 1;
-        cfg.attrs = attr; cfg.numAttrs = 1;
-    }
+    launch_config(cfg, attr, o.attr, o.grid, o.block, o.bytes, st);
     return cudaLaunchKernelExC(&cfg, o.func, params);
 }
 

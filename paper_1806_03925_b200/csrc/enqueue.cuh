@@ -86,6 +86,8 @@ cudaError_t enqueue_copy(void* dst, const void* src, size_t bytes, cudaStream_t 
 cudaError_t enqueue_record(cudaEvent_t ev, cudaStream_t st);
 cudaError_t enqueue_wait(cudaStream_t st, cudaEvent_t ev);
 cudaError_t launch_list_kernel(const Op& o, OpList& l, cudaStream_t st);
+// How a kernel is launched: grid, shared memory and the one attribute it may have (kept in attr, which cfg points to).
+void launch_config(cudaLaunchConfig_t& cfg, cudaLaunchAttribute (&attr)[1], Op::Attr kind, dim3 grid, dim3 block, size_t smem, cudaStream_t st);
 
 // Plays lists for one ctx and keeps its graphs (at most MAX_GRAPHS shapes; given back with the ctx).
 class Player {

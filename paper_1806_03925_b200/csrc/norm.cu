@@ -753,7 +753,7 @@ template <typename T, int C, bool RES> static bool back_stream_go(const NormArgs
     if (blocks < 1 || !stream_fits(a.n, blocks)) return false;
     *grid = sm_count() * blocks;
     *e = allow_smem<rms_norm_back_stream_kernel<T, C, RES>>(SMEM);
-    if (*e == cudaSuccess) *e = launch_dependent(rms_norm_back_stream_kernel<T, C, RES>, dim3((unsigned)*grid), dim3(32 * STREAM_WARPS), (size_t)SMEM, st, a);
+    if (*e == cudaSuccess) *e = launch_now(rms_norm_back_stream_kernel<T, C, RES>, dim3((unsigned)*grid), dim3(32 * STREAM_WARPS), (size_t)SMEM, st, a);
     return true;
 }
 template <typename T> static bool back_stream(const NormArgs& a, int* grid, cudaError_t* e, cudaStream_t st) {
@@ -764,7 +764,7 @@ template <typename T> static bool back_stream(const NormArgs& a, int* grid, cuda
 
 template <typename T, bool VEC, bool ONE, int C> static cudaError_t norm_go(const NormArgs& a, cudaStream_t st) {
     const int warps = ONE ? NORM_ROWS : (int)ceil_div(ceil_div(a.cols, Chunk<T, VEC>::COLS), C);
-    return launch_dependent(rms_norm_kernel<T, VEC, ONE, C>, dim3((unsigned)(ONE ? ceil_div(a.n, NORM_ROWS) : a.n)), dim3(32 * warps), 0, st, a);
+    return launch_now(rms_norm_kernel<T, VEC, ONE, C>, dim3((unsigned)(ONE ? ceil_div(a.n, NORM_ROWS) : a.n)), dim3(32 * warps), 0, st, a);
 }
 template <typename T, bool VEC> static cudaError_t norm_by_width(const NormArgs& a, cudaStream_t st) {
     constexpr int COLS = Chunk<T, VEC>::COLS;
@@ -791,7 +791,7 @@ template <typename T, bool VEC> static cudaError_t norm_by_width(const NormArgs&
     if (pieces <= 32) return norm_go<T, VEC, false, 4>(a, st);
     if constexpr (COLS == 128) { if (pieces <= 64) return norm_go<T, VEC, false, 8>(a, st); }
     const int64_t blocks = a.n < (int64_t)sm_count() * 8 ? a.n : (int64_t)sm_count() * 8;
-    return launch_dependent(rms_norm_wide_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, st, a);
+    return launch_now(rms_norm_wide_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, st, a);
 }
 
 // PER_SM: blocks of 256 threads that an SM takes (in registers); the grid is no larger than what runs at once.
@@ -800,7 +800,7 @@ template <typename T, bool VEC, int C, int PER_SM> static cudaError_t back_go(co
     *blocks = (int)(a.n < most ? a.n : most);
     if (*blocks > GEAR_NORM_WORKSPACE_ROWS) *blocks = GEAR_NORM_WORKSPACE_ROWS;
     const int warps = (int)ceil_div(ceil_div(a.cols, Chunk<T, VEC>::COLS), C);
-    return launch_dependent(rms_norm_back_kernel<T, VEC, C, PER_SM>, dim3((unsigned)*blocks), dim3(32 * warps), 0, st, a);
+    return launch_now(rms_norm_back_kernel<T, VEC, C, PER_SM>, dim3((unsigned)*blocks), dim3(32 * warps), 0, st, a);
 }
 template <typename T, bool VEC> static cudaError_t back_by_width(const NormArgs& a, int* blocks, cudaStream_t st) {
     constexpr int COLS = Chunk<T, VEC>::COLS;
@@ -816,7 +816,7 @@ template <typename T, bool VEC> static cudaError_t back_by_width(const NormArgs&
     if (pieces <= 32) return back_go<T, VEC, 4, 1>(a, blocks, st);
     if constexpr (COLS == 128) { if (pieces <= 64) return back_go<T, VEC, 8, 1>(a, blocks, st); }
     *blocks = (int)(a.n < GEAR_NORM_WORKSPACE_ROWS ? a.n : GEAR_NORM_WORKSPACE_ROWS);
-    return launch_dependent(rms_norm_back_wide_kernel<T>, dim3((unsigned)*blocks), dim3(256), 0, st, a);
+    return launch_now(rms_norm_back_wide_kernel<T>, dim3((unsigned)*blocks), dim3(256), 0, st, a);
 }
 
 cudaError_t launch_rms_norm(const NormArgs& a, int dtype, cudaStream_t st) {
@@ -832,14 +832,14 @@ cudaError_t launch_rms_norm_backward(const NormArgs& a, int dtype, cudaStream_t 
     if (dtype == GEAR_BF16) e = vectors(a, 2) ? back_by_width<__nv_bfloat16, true>(a, &blocks, st) : back_by_width<__nv_bfloat16, false>(a, &blocks, st);
     else e = vectors(a, 4) ? back_by_width<float, true>(a, &blocks, st) : back_by_width<float, false>(a, &blocks, st);
     if (e != cudaSuccess || !a.dweight) return e;
-    return launch_dependent(norm_dweight_kernel, dim3((unsigned)ceil_div(a.cols, 32)), dim3(1024), 0, st, static_cast<const float*>(a.parts), blocks,
+    return launch_now(norm_dweight_kernel, dim3((unsigned)ceil_div(a.cols, 32)), dim3(1024), 0, st, static_cast<const float*>(a.parts), blocks,
                             a.cols, a.dweight);
 }
 
 cudaError_t launch_q8_weights(const float* W, int64_t ldw, int K, int N, uint8_t* q, int64_t ldq, float* scale, uint8_t* qt, int64_t ldqt,
                               float* scale_t, cudaStream_t st) {
     const int vec = on16(W, ldw, 4);
-    return launch_dependent(q8_weights_kernel, dim3((unsigned)ceil_div(K, Q8_BLOCK), (unsigned)ceil_div(N, Q8_BLOCK)), dim3(QW_THREADS), 0, st,
+    return launch_now(q8_weights_kernel, dim3((unsigned)ceil_div(K, Q8_BLOCK), (unsigned)ceil_div(N, Q8_BLOCK)), dim3(QW_THREADS), 0, st,
                             W, ldw, vec, K, N, q, ldq, scale, qt, ldqt, scale_t);
 }
 

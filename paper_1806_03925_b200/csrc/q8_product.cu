@@ -438,10 +438,10 @@ template <int BN, typename T> static cudaError_t qp_go(const Q8Args& q, cudaStre
     const int64_t tiles = ceil_div(q.n, TC_BM) * g.n_tiles;
     if (tiles > INT32_MAX) return cudaErrorInvalidValue;     // (an output of 2^31 tiles fits no memory)
     const int grid = tiles < sm_count() ? (int)tiles : sm_count();
-    return launch_dependent(kernel, dim3(grid), dim3(QP_THREADS), (size_t)Cfg::SMEM, st, ma, mb, mo, g);
+    return launch_now(kernel, dim3(grid), dim3(QP_THREADS), (size_t)Cfg::SMEM, st, ma, mb, mo, g);
 }
 template <int R, typename T> static cudaError_t qf_go(const Q8Args& q, cudaStream_t st) {
-    return launch_dependent(q8_few_rows_kernel<R, T>, dim3((unsigned)ceil_div(q.N, 4), (unsigned)ceil_div(q.n, R)), dim3(128), 0, st, q);
+    return launch_now(q8_few_rows_kernel<R, T>, dim3((unsigned)ceil_div(q.N, 4), (unsigned)ceil_div(q.n, R)), dim3(128), 0, st, q);
 }
 
 template <typename T> static cudaError_t qp_launch(const Q8Args& q, cudaStream_t st) {
