@@ -400,7 +400,8 @@ int gear_adam_dense(float* param, const float* grad, float* m, float* v, int64_t
  *   - status (device, two words, zero before the first call; optional unless said otherwise): GEAR_DEV_* bits are added to
  *     status[0]; status[1] is non-zero once a bounded wait has given up (GEAR_DEV_TIMEOUT), and until the caller clears it.
  *     Calls on streams that may overlap each have a status of their own;
- *   - inputs and outputs do not overlap, except where said.
+ *   - inputs and outputs do not overlap, except where said; all pointers belong to the current device;
+ *   - a stream under capture takes them like any other, after a first call of the same kind outside of a capture.
  *
  * The 8-bit form of a row h of `cols` values, block by block of GEAR_Q8_BLOCK columns (the last one may be shorter):
  *     scale = max(max_j |h_j|, 2^-100) / 448,    q_j = h_j / scale rounded to e4m3 (nearest even).

@@ -2,7 +2,8 @@
 //     norm = sqrt(sum g^2),  c = min(1, max_norm / (norm + 1e-6)),  out = c g.
 // Two launches: every block leaves the sum of squares of its share of the values, then every block adds up all shares in one
 // order, which gives each of them the same c, and scales its own.  No atomics: the same list gives the same bits.
-// Bound by memory: a list that does not fit the L2 is read twice and written once.  The second launch walks a block's share
+// Bound by memory: a list that does not fit the L2 is read twice and written once (94 million values in 150 tensors, fp32 and bf16: 171 us for
+// 950 MB; blocks of 592 or 1184, four or eight loads ahead, eviction hints, shorter steps backwards are within 3 % of each other, forwards 174).  The second launch walks a block's share
 // backwards, so that it begins with what the first one has left in the L2.
 // Squares are formed and added in 64 bits: a gradient of 1e-30 or 1e30 has a norm too, and a sum of a billion terms keeps its digits.
 #include "common.cuh"
@@ -11,7 +12,7 @@
 namespace gear {
 
 constexpr int CLIP_THREADS = 256;
-constexpr int CLIP_BLOCKS = 1184;          // eight for every SM of a B200 (94 million values in 150 tensors: 166 us; four: 171): also the shares in the workspace
+constexpr int CLIP_BLOCKS = 1184;          // eight for every SM of a B200: also the shares in the workspace
 constexpr int CLIP_SMALL = 32, CLIP_MIDDLE = 256, CLIP_LARGE = 1024;      // tensors a launch can take, as kernel parameters (30 KB of them cost the host 5 us)
 constexpr uint32_t CLIP_BACK = 8;          // tiles of a step backwards
 static_assert(CLIP_BLOCKS * sizeof(double) <= GEAR_CLIP_WORKSPACE_BYTES, "workspace");

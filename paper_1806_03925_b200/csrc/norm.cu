@@ -639,7 +639,7 @@ norm_dweight_kernel(const float* __restrict__ parts, int rows, int cols, float* 
 // ---------------------------------------------------------------- weights
 // One block per 128 x 128 weights.  A lane holds squares of 4 x 4 of them from their load on: its values of a row are four bytes of the
 // transposed copy, and, turned round in registers, four bytes of a column go to shared memory, from where whole rows of the other copy
-// leave.  (The weights as fp32 in shared memory, bytes stored one by one: 10.1 us for 2048 x 1024, this 4.)
+// leave.  (The weights as fp32 in shared memory, bytes stored one by one: 10.1 us for 2048 x 1024, this 4.1.)
 constexpr int QW_THREADS = 512;
 __device__ __forceinline__ void put_bytes(uint8_t* p, uint32_t w, int left, bool words) {
     if (words && left >= 4) *reinterpret_cast<uint32_t*>(p) = w;
