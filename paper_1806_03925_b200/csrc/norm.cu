@@ -21,7 +21,7 @@ namespace gear {
 // (any alignment, any width; a warp's loads are still whole lines).
 template <typename T, bool VEC> struct Chunk;
 template <> struct Chunk<float, true> {
-    static constexpr int E = 4, COLS = 128, Q = 128;          // values, columns of the chunk
+    static constexpr int E = 4, COLS = 128;          // values, columns of the chunk
     float4 v;
     static __device__ __forceinline__ int col(int lane, int e) { return lane * 4 + e; }
     static __device__ __forceinline__ bool in(int lane, int, int left) { return lane * 4 < left; }      // (widths are multiples of E)
@@ -33,7 +33,7 @@ template <> struct Chunk<float, true> {
     __device__ __forceinline__ void set(const f32x2 (&f)[2]) { v = make_float4(low(f[0]), high(f[0]), low(f[1]), high(f[1])); }
 };
 template <> struct Chunk<__nv_bfloat16, true> {
-    static constexpr int E = 8, COLS = 256, Q = 128;
+    static constexpr int E = 8, COLS = 256;
     uint4 v;
     static __device__ __forceinline__ int col(int lane, int e) { return lane * 8 + e; }
     static __device__ __forceinline__ bool in(int lane, int, int left) { return lane * 8 < left; }
@@ -48,7 +48,7 @@ template <> struct Chunk<__nv_bfloat16, true> {
     __device__ __forceinline__ void set(const f32x2 (&f)[4]) { v = make_uint4(to_bf16x2(f[0]), to_bf16x2(f[1]), to_bf16x2(f[2]), to_bf16x2(f[3])); }
 };
 template <typename T> struct Chunk<T, false> {
-    static constexpr int E = 4, COLS = 128, Q = 128;
+    static constexpr int E = 4, COLS = 128;
     T v[4];
     static __device__ __forceinline__ int col(int lane, int e) { return lane + 32 * e; }
     static __device__ __forceinline__ bool in(int lane, int e, int left) { return lane + 32 * e < left; }

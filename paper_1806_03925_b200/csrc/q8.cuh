@@ -74,6 +74,5 @@ struct Q8Plain {
     __device__ __forceinline__ f32x2 operator()(f32x2 v) const { return pack2(low(v) * r / scale, high(v) * r / scale); }
 };
 __device__ __forceinline__ uint16_t q8_pair(f32x2 v) { return (uint16_t)__nv_cvt_float2_to_fp8x2(make_float2(low(v), high(v)), __NV_SATFINITE, __NV_E4M3); }
-__device__ __forceinline__ uint8_t q8_one(float v) { return (uint8_t)__nv_cvt_float_to_fp8(v, __NV_SATFINITE, __NV_E4M3); }
 
 }  // namespace gear
