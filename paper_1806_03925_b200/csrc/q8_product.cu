@@ -244,6 +244,7 @@ q8_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         // an accumulator is read in pieces of 32 columns, the next one on its way while one is added up: also across accumulators
         constexpr int WIDE = 32, PIECES = COLS / WIDE;
         Ring<ACCS> ring;
+        uint32_t sent = 0;                                    // groups of copies (or empty ones) the warp has committed, over all of its tiles
         bool ok = true;
         for (uint32_t t = blockIdx.x; t < total && ok; t += gridDim.x) {
             const uint32_t mt = t / n_tiles;
@@ -303,8 +304,10 @@ q8_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
 #pragma unroll
             for (int c = 0; c < (COLS + PIECE - 1) / PIECE; ++c) {
                 if (n0 + c * PIECE >= g.N) break;             // (uniform over the warp)
-                const uint32_t box = block + (uint32_t)(c % Cfg::OUT_BLOCKS) * QP_OUT_BLOCK;
-                if (lane == 0) tma_store_wait_read<Cfg::OUT_BLOCKS - 1>();      // the block's previous contents have been read (a copy is one group)
+                // the blocks in turn, across tiles: all groups but the last OUT_BLOCKS - 1 have been read, so this block's previous contents have
+                const uint32_t box = block + (sent % Cfg::OUT_BLOCKS) * QP_OUT_BLOCK;
+                ++sent;
+                if (lane == 0) tma_store_wait_read<Cfg::OUT_BLOCKS - 1>();
                 __syncwarp();
                 const uint32_t row = box + (uint32_t)lane * 128u;
 #pragma unroll

@@ -326,6 +326,21 @@ def test_product(gb, n, K, N, out_dtype):
     check_product(out, a, sa, b, sb)
 
 
+@pytest.mark.parametrize("out_dtype", [F32, BF16])
+@pytest.mark.parametrize("n,K,N", [(131_072, 16, 64), (131_072, 64, 64), (131_072, 128, 64), (100_003, 130, 36), (90_001, 256, 20), (200_000, 128, 52), (60_000, 16, 128),
+                                   (150_000, 40, 100), (80_000, 128, 256)])
+def test_product_many_tiles_a_block(gb, n, K, N, out_dtype):
+    """Several row tiles to every CTA at one or two blocks of K: a tile's results are put together while those of the one before it are
+    still leaving.  All rows, three times the same bits."""
+    a, sa, b, sb = q8_data(n, K, N, n + K + N)
+    st, outs = status(), [torch.full((n, N), 5.0, dtype=out_dtype, device="cuda") for _ in range(3)]
+    for o in outs:
+        gb.gear_q8_matmul(a, sa, b, sb, o, st)
+    assert st.tolist() == [0, 0]
+    check_product(outs[0], a, sa, b, sb)
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+
+
 @pytest.mark.parametrize("n,N", [(6, 72), (500, 64), (500, 1000), (30000, 256)])
 def test_product_rows_behind_the_live_ones(gb, n, N):
     """d_n on the device; rows behind it, columns beside the output and a row's misaligned start."""
