@@ -54,11 +54,28 @@ struct QpArgs {
 // the first one keeps 40 (256 x 232 + 128 x 40 = 64512).
 constexpr int QP_REGS_FEW = 40, QP_REGS_MANY = 232;
 
+// mbar_wait that looks more often whether another wait has given up: a block whose epilogue has left ends soon.
+__device__ __forceinline__ bool qp_wait(uint32_t bar, uint32_t parity, int32_t* err, int code) {
+    for (uint32_t i = 0; i < TC_SPIN_LIMIT; ++i) {
+        if (mbar_try(bar, parity)) return true;
+        if (i > 64) __nanosleep(32);
+        if ((i & 63u) == 63u && *reinterpret_cast<volatile int32_t*>(err) != 0) return false;
+    }
+    atomicCAS(err, 0, code);
+    return false;
+}
 // One lane waits for its warp.
 __device__ __forceinline__ bool qp_warp_wait(uint32_t bar, uint32_t parity, int32_t* err, int lane) {
     bool ok = true;
-    if (lane == 0) ok = mbar_wait(bar, parity, err, 4);
+    if (lane == 0) ok = qp_wait(bar, parity, err, 4);
     return __all_sync(0xffffffffu, ok);
+}
+// All threads of the block meet, each from its own role's code; whether any of them brings a true.
+__device__ __forceinline__ bool qp_any(bool mine) {
+    uint32_t any;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, 1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(any) : "r"((uint32_t)mine), "n"(QP_THREADS) : "memory");
+    return any != 0;
 }
 
 __device__ __forceinline__ uint64_t pair64(uint32_t lo, uint32_t hi) { return (uint64_t)lo | (uint64_t)hi << 32; }
@@ -171,18 +188,19 @@ q8_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
 
     if (warp < 4) {
         if (Cfg::SPLIT) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(QP_REGS_FEW));
+        uint32_t it = 0;                                                              // producers: blocks walked past
+        uint32_t last_full = 0, last_empty = 0, full_round = 0, empty_round = 0;      // issuers: the barriers of the last block issued
+        bool ok = true;
         // ---------------- TMA producers: two warps, every second block of K each (one alone took 690 cycles from block to block); the
         // whole warp walks the loop, so that what it counts stays in uniform registers, and one lane issues
         if (warp == 0 || warp == 3) {
             Ring<STAGES> ring;
-            uint32_t it = 0;
             const uint32_t odd = (uint32_t)(warp == 3);
-            bool ok = true;
             for (uint32_t t = blockIdx.x; t < total && ok; t += gridDim.x) {
                 const int mt = (int)(t / n_tiles), nt = (int)(t - (uint32_t)mt * n_tiles);      // the column tiles of a row tile side by side
                 for (int kb = 0; kb < kbs; ++kb, ++it, ring.next()) {
                     if ((it & 1u) != odd) continue;
-                    ok = __all_sync(0xffffffffu, mbar_wait(empty_bar(ring.at), ring.round ^ 1u, err, 1));
+                    ok = __all_sync(0xffffffffu, qp_wait(empty_bar(ring.at), ring.round ^ 1u, err, 1));
                     if (!ok) break;
                     const uint32_t a_dst = tiles + ring.at * Cfg::STAGE_BYTES, b_dst = a_dst + Cfg::A_BYTES, bar = full_bar(ring.at);
                     if (elect_one()) {
@@ -192,13 +210,6 @@ q8_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                     }
                     __syncwarp();
                 }
-            }
-            if (lane == 0 && *reinterpret_cast<volatile int32_t*>(err) != 0) {
-                // leaving early: let the copies already issued land before the CTA gives its shared memory back
-                const uint32_t first = it > (uint32_t)STAGES ? it - STAGES : 0u;
-                for (uint32_t j = first; j < it; ++j)
-                    for (uint32_t spin = 0; (j & 1u) == odd && spin < (1u << 16) && !mbar_try(full_bar(j % STAGES), (j / STAGES) & 1u); ++spin)
-                        __nanosleep(64);
             }
         }
         // ---------------- MMA issuers: two warps, every second block of K each (blocks have accumulators of their own, so the order
@@ -210,12 +221,10 @@ q8_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             Ring<STAGES> ring;
             Ring<ACCS> acc;
             uint32_t mine = (uint32_t)warp & 1u;
-            uint32_t last_full = 0, last_empty = 0, full_round = 0, empty_round = 0;      // the barriers of the last block issued
-            bool ok = true;
             for (uint32_t t = blockIdx.x; t < total && ok; t += gridDim.x) {
                 for (int kb = 0; kb < kbs; ++kb, ring.next(), acc.next(), mine ^= 1u) {
                     if (!mine) continue;
-                    ok = mbar_wait(full_bar(ring.at), ring.round, err, 3) && mbar_wait(acc_empty(acc.at), acc.round ^ 1u, err, 2);
+                    ok = qp_wait(full_bar(ring.at), ring.round, err, 3) && qp_wait(acc_empty(acc.at), acc.round ^ 1u, err, 2);
                     if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
                     tc_fence_after();
                     const uint64_t step = (uint64_t)(uint32_t)(ring.at * (Cfg::STAGE_BYTES >> 4));      // (addresses in a descriptor are in 16 bytes)
@@ -230,8 +239,17 @@ q8_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                     __syncwarp();
                 }
             }
-            // leaving early: what has been issued ends before the CTA gives its tensor memory and barriers back
-            if (!ok && last_full != 0)
+        }
+        // If any wait of the block gave up, in whatever role and however late, copies and products may be under way that nobody has waited
+        // for: they land and end before the CTA gives its shared memory, its barriers and its tensor memory back.
+        if (qp_any(!ok)) {
+            if ((warp == 0 || warp == 3) && lane == 0) {
+                const uint32_t first = it > (uint32_t)STAGES ? it - STAGES : 0u, odd = (uint32_t)(warp == 3);
+                for (uint32_t j = first; j < it; ++j)
+                    for (uint32_t spin = 0; (j & 1u) == odd && spin < (1u << 16) && !mbar_try(full_bar(j % STAGES), (j / STAGES) & 1u); ++spin)
+                        __nanosleep(64);
+            }
+            if (last_full != 0)
                 for (uint32_t spin = 0; spin < (1u << 16) && !(mbar_try(last_full, full_round) && mbar_try(last_empty, empty_round)); ++spin)
                     __nanosleep(64);
         }
@@ -245,8 +263,10 @@ q8_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         constexpr int WIDE = 32, PIECES = COLS / WIDE;
         Ring<ACCS> ring;
         uint32_t sent = 0;                                    // groups of copies (or empty ones) the warp has committed, over all of its tiles
+        // (a status that an earlier call has left says that this call's results are void: none are written)
+        const uint32_t start = __shfl_sync(0xffffffffu, *reinterpret_cast<volatile int32_t*>(err) == 0 ? blockIdx.x : total, 0);
         bool ok = true;
-        for (uint32_t t = blockIdx.x; t < total && ok; t += gridDim.x) {
+        for (uint32_t t = start; t < total && ok; t += gridDim.x) {
             const uint32_t mt = t / n_tiles;
             const int nt = (int)(t - mt * n_tiles);
             const int64_t m0 = (int64_t)mt * TC_BM + quarter * 32, m = m0 + lane;
@@ -342,6 +362,7 @@ q8_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             }
         }
         if (lane == 0) tma_store_wait_all();
+        qp_any(!ok || start >= total);
     }
 
     tc_fence_before();

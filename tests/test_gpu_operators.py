@@ -435,6 +435,27 @@ def test_product_says_that_a_wait_gave_up(gb):
     check_product(out, a, sa, b, sb)
 
 
+@pytest.mark.parametrize("out_dtype", [F32, BF16])
+@pytest.mark.parametrize("n,K,N", [(40_000, 1040, 256), (20_000, 144, 520), (131_072, 64, 64), (50_000, 300, 100), (20_000, 2048, 1024), (200, 16, 300)])
+def test_product_ends_whole_after_an_early_exit(gb, n, K, N, out_dtype):
+    """The epilogue leaves at once, with the operands' copies and the first products under way; the waits of the others give up.  The call
+    says so, writes nothing, and the calls behind it, with a clear status, are whole."""
+    a, sa, b, sb = q8_data(n, K, N, n + K + N)
+    want, out = torch.empty((n, N), dtype=out_dtype, device="cuda"), torch.full((n, N), 5.0, dtype=out_dtype, device="cuda")
+    gb.gear_q8_matmul(a, sa, b, sb, want, status())
+    check_product(want, a, sa, b, sb)
+    for _ in range(3):
+        st = torch.tensor([0, 3], dtype=torch.int32, device="cuda")
+        for _ in range(2):
+            gb.gear_q8_matmul(a, sa, b, sb, out, st)
+        assert st.tolist() == [gb_timeout, 3]
+        assert (out == 5.0).all()
+        st.zero_()
+        got = torch.empty_like(out)
+        gb.gear_q8_matmul(a, sa, b, sb, got, st)
+        assert st.tolist() == [0, 0] and torch.equal(got, want)
+
+
 def test_product_results_beyond_32_bits(gb):
     n, K, N = (1 << 31) // 1024 + 300, 48, 1024
     a, b = torch.zeros((n, K), dtype=torch.uint8, device="cuda").view(E4M3), e4m3_rows(N, K)
