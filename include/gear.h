@@ -452,7 +452,9 @@ int gear_q8_weights(const float* W, int64_t ldw, int32_t K, int32_t N, void* q, 
 
 /*
  * out[m][j] = sum_kb a_scale[m][kb] b_scale[j / 128][kb] (sum over k of block kb of a[m][k] b[j][k]),  m < n, j < N, blocks of 128 along K.
- * a [n][lda], b [N][ldb] e4m3, 16-byte aligned, lda and ldb multiples of 16 (what lies in a row behind K is not used);
+ * a [n][lda], b [N][ldb] e4m3, 16-byte aligned, lda and ldb multiples of 16.  Rows are read in aligned words of 16 bytes, up to
+ * the one that holds value K - 1, the last row's too (a word that begins in an allocation of the CUDA runtime or of a framework on top of it ends
+ * in it); what it holds behind K is not used.
  * a_scale [n][ceil(K / 128)], b_scale [ceil(N / 128)][ceil(K / 128)].  out_dtype GEAR_F32 or GEAR_BF16.  Products are exact, sums fp32.
  * Scales and products outside fp32's range become infinities or zeros as fp32 has it.  status: required.
  */

@@ -584,7 +584,8 @@ def gear_q8_matmul(a, a_scale, b, b_scale, out, status, n: Optional[int] = None,
     K = a.shape[1]
     if b.shape != (N, K):
         _refuse("b has the shape %s; needed: %d x %d" % (tuple(b.shape), N, K))
-    if n == 1:                                       # (a single row's distance to the next one does not matter)
+    if n == 1:                                       # (a single row's distance to the next one does not matter; its last 16-byte word is read
+                                                     # whole, which torch's allocations, of 512 bytes and more, always hold)
         lda = (lda + 15) & ~15
     if N == 1:
         ldb = (ldb + 15) & ~15

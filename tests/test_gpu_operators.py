@@ -379,6 +379,22 @@ def test_product_of_what_is_not_finite(gb):
         assert (off <= size[:, keep] * 135 * 2.0 ** -23).all()
 
 
+@pytest.mark.parametrize("n", [1, 3, 8])
+def test_product_of_rows_that_end_with_their_memory(gb, n):
+    """Every remainder of K by 16, in tensors that end with the last row's last value, and with NaN behind every row."""
+    for K in list(range(1, 18)) + [100, 127, 499, 1535]:
+        N, ld = 40, (K + 15) // 16 * 16
+        a, sa, b, sb = q8_data(n, K, N, K)
+        ends = [torch.full(((t.shape[0] - 1) * ld + K,), 0x7f, dtype=torch.uint8, device="cuda").view(E4M3).as_strided(t.shape, (ld, 1)) for t in (a, b)]
+        ends[0].copy_(a)
+        ends[1].copy_(b)
+        out, same = torch.full((n, N), 5.0, device="cuda"), torch.full((n, N), 6.0, device="cuda")
+        gb.gear_q8_matmul(ends[0], sa, ends[1], sb, out, status())
+        gb.gear_q8_matmul(a, sa, b, sb, same, status())
+        check_product(out, a, sa, b, sb)
+        assert torch.equal(out, same)
+
+
 def test_product_repeats(gb):
     a, sa, b, sb = q8_data(7000, 1536, 256, 21)
     outs = [torch.empty((7000, 256), device="cuda") for _ in range(3)]
