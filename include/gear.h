@@ -395,7 +395,7 @@ int gear_adam_dense(float* param, const float* grad, float* m, float* v, int64_t
  * 128 x 128 of them.  A layer is gear_rms_norm, then gear_q8_matmul; the last product's fp32 rows are what gear_refresh_dfv takes.
  * These calls need no ctx.  General to them:
  *   - a row k stands at ptr + k * ld (ld in elements, at least the number of columns); any alignment of an element's own size and
- *     any ld will do unless said otherwise (16-byte aligned rows are read and written faster);
+ *     any ld will do unless said otherwise (16-byte aligned rows are read and written faster); a row has at most 2^31 - 1024 columns;
  *   - d_n (device, optional): only rows k < min(n, *d_n) are computed, *d_n read when the kernel runs; the others stay as they were;
  *   - status (device, two words, zero before the first call; optional unless said otherwise): GEAR_DEV_* bits are added to
  *     status[0]; status[1] is non-zero once a bounded wait has given up (GEAR_DEV_TIMEOUT), and until the caller clears it: until

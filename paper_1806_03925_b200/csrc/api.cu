@@ -939,11 +939,14 @@ int gear_adam_dense(float* param, const float* grad, float* m, float* v, int64_t
 static int dtype_size(int32_t dtype) { return dtype == GEAR_E4M3 ? 1 : dtype == GEAR_BF16 ? 2 : 4; }
 static bool aligned_to(const void* p, int32_t dtype) { return reinterpret_cast<uintptr_t>(p) % (uintptr_t)dtype_size(dtype) == 0; }
 
+// Longest rows: the kernels step over a row's columns in 32-bit numbers, at most 1024 columns at a time.
+constexpr int32_t MAX_COLS = INT32_MAX - 1023;
+
 // what gear_rms_norm and its gradients share
 static int check_norm(const NormArgs& a, int32_t dtype) {
     if (dtype != GEAR_F32 && dtype != GEAR_BF16) return arg_fail("dtype: GEAR_F32 or GEAR_BF16");
     if (a.n < 0 || a.n > INT32_MAX) return arg_fail("n outside [0, 2^31 - 1]");
-    if (a.cols < 1) return arg_fail("cols >= 1");
+    if (a.cols < 1 || a.cols > MAX_COLS) return arg_fail("cols outside [1, 2^31 - 1024]");
     if (!(a.eps >= 0.f)) return arg_fail("eps >= 0");
     if (a.ids && (a.vocab < 1 || a.vocab > INT32_MAX)) return arg_fail("vocab outside [1, 2^31 - 1]");
     if (a.n > 0 && (!a.x || a.ldx < a.cols || !aligned_to(a.x, dtype))) return arg_fail("x: NULL, misaligned or ldx < cols");
@@ -1003,7 +1006,8 @@ int gear_rms_norm_backward(const void* x, int64_t ldx, int32_t dtype, const int3
 
 int gear_q8_weights(const float* W, int64_t ldw, int32_t K, int32_t N, void* q, int64_t ldq, float* scale, void* q_t, int64_t ldq_t,
                     float* scale_t, void* stream) {
-    if (K < 1 || N < 1 || !W || ldw < N || !aligned_to(W, GEAR_F32)) return arg_fail("K, N >= 1; W: NULL, misaligned or ldw < N");
+    if (K < 1 || N < 1 || K > MAX_COLS || N > MAX_COLS) return arg_fail("K, N outside [1, 2^31 - 1024]");
+    if (!W || ldw < N || !aligned_to(W, GEAR_F32)) return arg_fail("W: NULL, misaligned or ldw < N");
     if ((!q && !q_t) || (q && (!scale || ldq < K)) || (q_t && (!scale_t || ldq_t < N))) return arg_fail("q, q_t: one of them, each with its scales, rows long enough");
     return finish(no_throw([&] {
         return launch_q8_weights(W, ldw, K, N, static_cast<uint8_t*>(q), ldq, scale, static_cast<uint8_t*>(q_t), ldq_t, scale_t, static_cast<cudaStream_t>(stream));
@@ -1012,7 +1016,7 @@ int gear_q8_weights(const float* W, int64_t ldw, int32_t K, int32_t N, void* q, 
 
 int gear_q8_matmul(const void* a, int64_t lda, const float* a_scale, const void* b, int64_t ldb, const float* b_scale, int64_t n,
                    const int64_t* d_n, int32_t N, int32_t K, void* out, int64_t ld_out, int32_t out_dtype, int32_t* status, void* stream) {
-    if (n < 0 || n > INT32_MAX - 128 || N < 1 || K < 1) return arg_fail("n in [0, 2^31 - 129], N, K >= 1");
+    if (n < 0 || n > INT32_MAX - 128 || N < 1 || K < 1 || N > MAX_COLS || K > MAX_COLS) return arg_fail("n outside [0, 2^31 - 129], N or K outside [1, 2^31 - 1024]");
     if (out_dtype != GEAR_F32 && out_dtype != GEAR_BF16) return arg_fail("out_dtype: GEAR_F32 or GEAR_BF16");
     if (!status) return arg_fail("status: required");
     if (n == 0) return GEAR_OK;

@@ -51,6 +51,19 @@ def test_refusals(gb, name, base, wrong):
             assert fn(*dict(b, n=0).values()) == gb.GEAR_OK         # nothing to do, nothing looked at
 
 
+def test_rows_too_long_to_step_over_are_refused(gb):
+    """Columns are counted in 32 bits, in steps of up to 1024: the numbers of longer rows would wrap around."""
+    L, far = gb.load(), 1 << 32
+    for cols in ((1 << 31) - 1023, (1 << 31) - 512, (1 << 31) - 1):
+        for name, base, long in (("gear_rms_norm", NORM, dict(cols=cols, ldx=far, ld_out=far)),
+                                 ("gear_rms_norm_backward", BACK, dict(cols=cols, ldx=far, ld_dout=far, ld_dx=far)),
+                                 ("gear_q8_rows", ROWS, dict(cols=cols, ldx=far, ldq=far)),
+                                 ("gear_q8_weights", WEIGHTS, dict(K=cols, ldq=far)), ("gear_q8_weights", WEIGHTS, dict(N=cols, ldw=far, ldq_t=far)),
+                                 ("gear_q8_matmul", MATMUL, dict(K=cols, lda=far, ldb=far)), ("gear_q8_matmul", MATMUL, dict(N=cols, ld_out=far))):
+            assert getattr(L, name)(*dict(base, **long).values()) == gb.GEAR_ERR_ARG, (name, long)
+            assert b"bad argument" in L.gear_last_error()
+
+
 def test_refusals_of_gradient_lists(gb):
     L = gb.load()
 
