@@ -1009,6 +1009,7 @@ int gear_q8_weights(const float* W, int64_t ldw, int32_t K, int32_t N, void* q, 
     if (K < 1 || N < 1 || K > MAX_COLS || N > MAX_COLS) return arg_fail("K, N outside [1, 2^31 - 1024]");
     if (!W || ldw < N || !aligned_to(W, GEAR_F32)) return arg_fail("W: NULL, misaligned or ldw < N");
     if ((!q && !q_t) || (q && (!scale || ldq < K)) || (q_t && (!scale_t || ldq_t < N))) return arg_fail("q, q_t: one of them, each with its scales, rows long enough");
+    if ((q && !aligned_to(scale, GEAR_F32)) || (q_t && !aligned_to(scale_t, GEAR_F32))) return arg_fail("scale, scale_t: misaligned");
     return finish(no_throw([&] {
         return launch_q8_weights(W, ldw, K, N, static_cast<uint8_t*>(q), ldq, scale, static_cast<uint8_t*>(q_t), ldq_t, scale_t, static_cast<cudaStream_t>(stream));
     }), "q8_weights");

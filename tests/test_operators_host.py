@@ -64,6 +64,12 @@ def test_rows_too_long_to_step_over_are_refused(gb):
             assert b"bad argument" in L.gear_last_error()
 
 
+def test_misaligned_scales_of_weights_are_refused(gb):
+    for wrong in (dict(scale=P + 2), dict(scale_t=P + 1), dict(q=None, scale_t=P + 2), dict(q_t=None, scale=P + 3)):
+        assert gb.load().gear_q8_weights(*dict(WEIGHTS, **wrong).values()) == gb.GEAR_ERR_ARG, wrong
+        assert b"scale" in gb.load().gear_last_error()
+
+
 def test_refusals_of_gradient_lists(gb):
     L = gb.load()
 
