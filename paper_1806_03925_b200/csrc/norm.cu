@@ -416,7 +416,7 @@ rms_norm_back_kernel(const NormArgs a) {
             for (int v = 0; v < warps; ++v) { sum.x += scratch[odd][v].x; sum.y += scratch[odd][v].y; }
         }
         const float r = 1.0f / sqrtf(sum.x * inv_cols + a.eps);
-        const float q = r * r * (sum.y * inv_cols);            // dx = r (g - y q): r alone may be large where y is small
+        const float q = r * (r * (sum.y * inv_cols));          // dx = r (g - y q): r alone may be large where y is small, and r r not a number
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             f32x2 f[H], d[H], o[H];
@@ -514,7 +514,7 @@ rms_norm_back_stream_kernel(const NormArgs a) {
         }
         const float sq = warp_sum(low(sq2) + high(sq2)), dot = warp_sum(low(dot2) + high(dot2));
         const float r = 1.0f / sqrtf(sq * inv_cols + a.eps);
-        const float q = r * r * (dot * inv_cols);
+        const float q = r * (r * (dot * inv_cols));
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int left = a.cols - c * Ch::COLS;
@@ -575,7 +575,7 @@ rms_norm_back_wide_kernel(const NormArgs a) {
         f32x2 sq2 = 0ull, dot2 = 0ull;
         for (int pass = 0; pass < 2; ++pass) {
             const float inv_cols = 1.0f / (float)a.cols;
-            const float r = 1.0f / sqrtf(sq * inv_cols + a.eps), q = r * r * (dot * inv_cols);      // (second pass)
+            const float r = 1.0f / sqrtf(sq * inv_cols + a.eps), q = r * (r * (dot * inv_cols));    // (second pass)
             for (int col0 = part * Ch::COLS; col0 < a.cols; col0 += 8 * Ch::COLS) {
                 const int left = a.cols - col0;
                 Ch y, g;

@@ -143,3 +143,27 @@ def test_gradients_of_what_is_not_finite(gb, n, cols, dtype, res):
     dw64 = back_exact(x, w, g, eps, None)[1]
     assert torch.equal(dw.isnan(), dw64.isnan()) and torch.equal(dw.isinf(), dw64.isinf())
     assert dw.isnan().sum() == 2 and dw.isinf().sum() == 1
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,cols", [(3, 64), (40, 1000), (40, 1001), (6000, 128), (6000, 1000), (6, 33_000)])
+def test_gradients_of_very_small_rows(gb, n, cols, dtype):
+    """Rows of zeros and of 1e-20 with an eps below what fp32 squares keep: r is 2e19 and more, its square beyond fp32, the gradients are not."""
+    g, w, ws = randn((n, cols), 1, dtype), 1 + 0.3 * randn((cols,), 2), torch.empty((gb.GEAR_NORM_WORKSPACE_ROWS, cols), device="cuda")
+    for x, eps in ((torch.zeros((n, cols), dtype=dtype, device="cuda"), 1e-40), (randn((n, cols), 3, dtype) * 4e-20, 0.0), (randn((n, cols), 3, dtype) * 4e-20, 1e-39)):
+        eps = float(torch.tensor(eps, dtype=F32))
+        dx, dw = torch.empty_like(x), torch.empty(cols, device="cuda")
+        gb.gear_rms_norm_backward(x, w, g, dx, dw, ws, eps)
+        want, dw64 = back_exact(x, w, g, eps, None)
+        xd, gd = x.double(), g.double() * w.double()
+        r = rms(xd, eps)
+        # beside the roundings of rows of usual size: what lies below 2^-126 is a multiple of 2^-149, off by 2^-150.  A sum of cols squares and of
+        # the lanes' and warps' sums (64 and fewer) has that for each, so their mean is off by (1 + 64 / cols) 2^-150, and by 2^-150 each for the product with 1 / cols and
+        # for eps, relative to mean + eps = 1 / r^2; half of it goes into r, which dx has to the third power.
+        k = cols / 32 + 16
+        small = (3 + 64 / cols) * 2.0 ** -150 * r ** 2
+        size = gd.abs() * r + xd.abs() * r ** 3 * (gd * xd).abs().mean(1, keepdim=True)
+        allowed = size * (3 * rms_rel(cols) + (k + 8) * U32 + 1.6 * small) + (0 if dtype == F32 else want.abs() * 2.0 ** -8 * 1.01)
+        assert ((dx.double() - want).abs() <= allowed).all()
+        size = (g.double() * xd).abs() * r
+        assert ((dw.double() - dw64).abs() <= (size * (rms_rel(cols) + (n / 592 + 110) * U32 + 0.6 * small)).sum(0) + 1e-44).all()
