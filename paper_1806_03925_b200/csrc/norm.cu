@@ -654,7 +654,10 @@ q8_weights_kernel(const float* __restrict__ W, int64_t ldw, int vec, int K, int 
     wait_for_predecessor();
     constexpr int SQUARES = Q8_BLOCK / 4 / (QW_THREADS / 32);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int k0 = blockIdx.x * Q8_BLOCK, n0 = blockIdx.y * Q8_BLOCK, kn = min(Q8_BLOCK, K - k0), nn = min(Q8_BLOCK, N - n0);
+    // (one number for both: a grid's second dimension ends at 65535)
+    const unsigned k_blocks = (unsigned)(K + Q8_BLOCK - 1) / Q8_BLOCK, n_blocks = (unsigned)(N + Q8_BLOCK - 1) / Q8_BLOCK;
+    const unsigned nb = blockIdx.x / k_blocks, kb = blockIdx.x - nb * k_blocks;
+    const int k0 = (int)kb * Q8_BLOCK, n0 = (int)nb * Q8_BLOCK, kn = min(Q8_BLOCK, K - k0), nn = min(Q8_BLOCK, N - n0);
     float4 v[SQUARES][4];
     float mine = 0.f;
 #pragma unroll
@@ -689,8 +692,8 @@ q8_weights_kernel(const float* __restrict__ W, int64_t ldw, int vec, int K, int 
     const Q8Plain plain(largest, 1.f);
     if (threadIdx.x == 0) {
         const float s = usual ? q8_usual_scale(largest, 1.f) : plain.scale;
-        if (q) scale[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = s;
-        if (qt) scale_t[(int64_t)blockIdx.x * gridDim.y + blockIdx.y] = s;
+        if (q) scale[(int64_t)nb * k_blocks + kb] = s;
+        if (qt) scale_t[(int64_t)kb * n_blocks + nb] = s;
     }
     const bool words_t = (reinterpret_cast<uintptr_t>(qt) & 3u) == 0 && (ldqt & 3) == 0, words = (reinterpret_cast<uintptr_t>(q) & 3u) == 0 && (ldq & 3) == 0;
 #pragma unroll
@@ -839,8 +842,9 @@ cudaError_t launch_rms_norm_backward(const NormArgs& a, int dtype, cudaStream_t 
 cudaError_t launch_q8_weights(const float* W, int64_t ldw, int K, int N, uint8_t* q, int64_t ldq, float* scale, uint8_t* qt, int64_t ldqt,
                               float* scale_t, cudaStream_t st) {
     const int vec = on16(W, ldw, 4);
-    return launch_now(q8_weights_kernel, dim3((unsigned)ceil_div(K, Q8_BLOCK), (unsigned)ceil_div(N, Q8_BLOCK)), dim3(QW_THREADS), 0, st,
-                            W, ldw, vec, K, N, q, ldq, scale, qt, ldqt, scale_t);
+    const int64_t blocks = ceil_div(K, Q8_BLOCK) * ceil_div(N, Q8_BLOCK);
+    if (blocks > INT32_MAX) return cudaErrorInvalidValue;    // (weights of 2^31 blocks fit no memory)
+    return launch_now(q8_weights_kernel, dim3((unsigned)blocks), dim3(QW_THREADS), 0, st, W, ldw, vec, K, N, q, ldq, scale, qt, ldqt, scale_t);
 }
 
 }  // namespace gear

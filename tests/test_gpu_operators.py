@@ -286,6 +286,20 @@ def test_weights(gb, K, N):
     assert torch.equal(only_t.float(), qt.float()) and torch.equal(only_st, st)
 
 
+@pytest.mark.parametrize("K,N", [(1, 8_400_001), (130, 8_388_500), (8_400_001, 1)])
+def test_weights_with_one_side_very_long(gb, K, N):
+    """More than 65535 blocks of 128 along a side."""
+    W = randn((K, N), 1)
+    q, s, qt, st = e4m3_rows(N, K), torch.empty((blocks(N), blocks(K)), device="cuda"), e4m3_rows(K, N), torch.empty((blocks(K), blocks(N)), device="cuda")
+    gb.gear_q8_weights(W, q, s, qt, st)
+    assert torch.equal(s, st.t())
+    for k0, n0 in ((0, 0), (0, max(0, (N - 1) // BLOCK * BLOCK)), (max(0, (K - 1) // BLOCK * BLOCK), 0), (K // 2 // BLOCK * BLOCK, N // 2 // BLOCK * BLOCK)):
+        w, b, t = W[k0:k0 + BLOCK, n0:n0 + BLOCK].double(), q[n0:n0 + BLOCK, k0:k0 + BLOCK].double(), qt[k0:k0 + BLOCK, n0:n0 + BLOCK].double()
+        scale, want = float(s[n0 // BLOCK, k0 // BLOCK]), float(w.abs().max()) / 448
+        assert abs(scale - want) <= want * 2 * U32 and torch.equal(b, t.t())
+        assert ((t * scale - w).abs() <= torch.maximum(w.abs() * 2.0 ** -4, torch.tensor(scale * 2.0 ** -10, device="cuda")) * (1 + 2.0 ** -10) + w.abs() * 5 * U32).all()
+
+
 # ------------------------------------------------------------------------------------------------ products
 def q8_data(n, K, N, seed, fill=0x7f):
     """Random operands; what lies behind K in a row is NaN, which no result may see."""
