@@ -608,6 +608,10 @@ class GradList:
 def make_grads(grads: Sequence[torch.Tensor], outs: Optional[Sequence[torch.Tensor]] = None) -> GradList:
     """The list gear_grad_norm and gear_clip_grads take, made once by a program whose gradients stay where they are.  outs: where the
     clipped gradients go (default: in place)."""
+    return _list_grads(grads, outs, True)
+
+
+def _list_grads(grads, outs, written_to: bool) -> GradList:
     where = grads if outs is None else outs
     if len(where) != len(grads):
         _refuse("as many outs as grads")
@@ -623,7 +627,7 @@ def make_grads(grads: Sequence[torch.Tensor], outs: Optional[Sequence[torch.Tens
             _refuse("takes device memory of the current device")
         if not (g.is_contiguous() and o.is_contiguous()):
             _refuse("takes contiguous gradients")
-        if g.numel() and to in written:
+        if written_to and g.numel() and to in written:
             _refuse("a gradient is written twice")
         written.add(to)
         l.items[i] = (at, to, g.numel(), code)
@@ -643,7 +647,7 @@ def gear_grad_norm(grads, norm, workspace, stream=None):
     """norm[0] = the 2-norm of all gradients together (a list of tensors, or what make_grads returned)."""
     dev = _device()
     if not isinstance(grads, GradList):
-        grads = make_grads(grads, grads)
+        grads = _list_grads(grads, None, False)
     l = _grads(grads)
     rc = (_lib or load()).gear_grad_norm(l.items, l.count, _vec(norm, torch.float32, dev, 1), _clip_workspace(workspace, dev),
                                          _current_stream(dev) if stream is None else _stream_here(stream, dev))

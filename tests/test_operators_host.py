@@ -87,6 +87,21 @@ def test_refusals_of_gradient_lists(gb):
     assert L.gear_clip_grads(None, 1, 1.0, P, P, None) == gb.GEAR_ERR_ARG
 
 
+def test_a_norm_of_the_same_gradient_twice(gb, monkeypatch):
+    """Nothing is written, so nothing is written twice: the sum has the gradient's squares twice."""
+    class Library:
+        def gear_grad_norm(self, items, count, norm, workspace, stream):
+            self.seen = [(items[i].grad, items[i].n) for i in range(count)]
+            return gb.GEAR_OK
+    lib = Library()
+    monkeypatch.setattr(gb, "_lib", lib)
+    monkeypatch.setattr(gb, "_device", lambda: -1)
+    monkeypatch.setattr(gb, "_current_stream", lambda dev: 0)
+    g = torch.ones(10)
+    gb.gear_grad_norm([g, g, g[2:5]], torch.zeros(2), torch.empty(gb.GEAR_CLIP_WORKSPACE_BYTES, dtype=torch.uint8))
+    assert lib.seen == [(g.data_ptr(), 10), (g.data_ptr(), 10), (g.data_ptr() + 8, 3)]
+
+
 def test_struct_layout_of_gradient_lists(gb, tmp_path):
     import os
     import shutil
