@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional, Sequence
 
 import torch
@@ -600,6 +601,9 @@ def gear_q8_matmul(a, a_scale, b, b_scale, out, status, n: Optional[int] = None,
         _check(rc, "gear_q8_matmul")
 
 
+_put_grad, _grad_size = struct.Struct("@PPqi4x").pack_into, C.sizeof(gear_grad)      # (a gear_grad; an assignment of its fields takes several times as long)
+
+
 class GradList:
     """The C form of a list of gradients (make_grads); keeps the tensors alive."""
     __slots__ = ("items", "count", "device", "tensors")
@@ -607,7 +611,7 @@ class GradList:
 
 def make_grads(grads: Sequence[torch.Tensor], outs: Optional[Sequence[torch.Tensor]] = None) -> GradList:
     """The list gear_grad_norm and gear_clip_grads take, made once by a program whose gradients stay where they are.  outs: where the
-    clipped gradients go (default: in place)."""
+    clipped gradients go (default: in place); an out is its gradient or overlaps nothing else of the list."""
     return _list_grads(grads, outs, True)
 
 
@@ -618,19 +622,30 @@ def _list_grads(grads, outs, written_to: bool) -> GradList:
     l = GradList()
     l.device = _device()
     l.items, l.count, l.tensors = (gear_grad * max(1, len(grads)))(), len(grads), (list(grads), list(where))
-    written = set()
+    spans = []                                       # (begin, end, whether it is written) of all memory of the call
     for i, (g, o) in enumerate(zip(grads, where)):
-        code, at, to = _FLOATS.get(g.dtype), g.data_ptr(), o.data_ptr()
-        if code is None or o.dtype != g.dtype or o.numel() != g.numel():
+        code, at, n = _FLOATS.get(g.dtype), g.data_ptr(), g.numel()
+        to = at if o is g else o.data_ptr()
+        if code is None or (o is not g and (o.dtype != g.dtype or o.numel() != n)):
             _refuse("gradients are fp32 or bf16, each out like its gradient")
-        if g.get_device() != l.device or o.get_device() != l.device:
+        if g.get_device() != l.device or (o is not g and o.get_device() != l.device):
             _refuse("takes device memory of the current device")
-        if not (g.is_contiguous() and o.is_contiguous()):
+        if not (g.is_contiguous() and (o is g or o.is_contiguous())):
             _refuse("takes contiguous gradients")
-        if written_to and g.numel() and to in written:
-            _refuse("a gradient is written twice")
-        written.add(to)
-        l.items[i] = (at, to, g.numel(), code)
+        if n and written_to:
+            size = n * (4 if code == GEAR_F32 else 2)
+            spans.append((to, to + size, True))
+            if at != to:
+                spans.append((at, at + size, False))
+        _put_grad(l.items, i * _grad_size, at, to, n, code)
+    read = written = 0                               # ends of what has been seen so far
+    for begin, end, out in sorted(spans):
+        if begin < written or (out and begin < read):
+            _refuse("a gradient is written twice, or what is written overlaps another tensor of the list")
+        if out:
+            written = max(written, end)
+        else:
+            read = max(read, end)
     return l
 
 

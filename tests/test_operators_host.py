@@ -102,6 +102,27 @@ def test_a_norm_of_the_same_gradient_twice(gb, monkeypatch):
     assert lib.seen == [(g.data_ptr(), 10), (g.data_ptr(), 10), (g.data_ptr() + 8, 3)]
 
 
+def test_overlapping_gradients_are_refused(gb, monkeypatch):
+    """What is written may be its own gradient, whole, and nothing else of the call."""
+    monkeypatch.setattr(gb, "_device", lambda: -1)
+    flat, back = torch.zeros(100), torch.zeros(100)
+    for grads, outs in (([flat[:10], flat[9:20]], None), ([flat[9:20], flat[:10]], None), ([flat, flat[50:60]], None), ([flat[:50], flat[3:4], flat[60:]], None),
+                        ([flat[:10], flat[10:20]], [back[:10], back[9:19]]), ([flat[:10]], [flat[1:11]]), ([flat[:10], flat[10:20]], [flat[10:20], flat[:10]]),
+                        ([flat[:10], flat[20:30]], [flat[20:30], back[:10]]), ([flat[:10], flat[:10]], [back[:10], back[:10]]),
+                        ([flat[:10], flat[2:4]], [flat[:10], back[:2]])):
+        with pytest.raises(TypeError, match="overlap|written twice"):
+            gb.make_grads(grads, outs)
+    half = flat.view(torch.bfloat16)
+    with pytest.raises(TypeError, match="overlap|written twice"):
+        gb.make_grads([flat[:10], half[19:30]])
+    for grads, outs in (([flat[:10], flat[10:20], flat[20:]], None), ([flat[10:20], flat[:10], flat[:0], flat[5:5]], None), ([flat[:10], flat[5:15]], [back[:10], back[10:20]]),
+                        ([flat[:10], half[20:30]], None), ([flat[:10], flat[20:30]], [flat[:10], flat[40:50]]), ([], None), ([flat[:0], flat[:0]], None)):
+        l = gb.make_grads(grads, outs)
+        assert l.count == len(grads)
+        for i, (g, o) in enumerate(zip(grads, outs or grads)):
+            assert (l.items[i].grad or 0, l.items[i].out or 0, l.items[i].n) == (g.data_ptr(), o.data_ptr(), g.numel())
+
+
 def test_struct_layout_of_gradient_lists(gb, tmp_path):
     import os
     import shutil
