@@ -24,7 +24,7 @@ def e4m3_rows(n: int, cols: int, device="cuda") -> torch.Tensor:
 
 class NormedDensePart:
     """raw: [img_vocab][raw_dim] fp32 or bf16; Wd: [raw_dim][dfv_dim] fp32 and weight: [raw_dim] fp32, both updated in place by step.
-    max_rows: most rows of one forward or backward call (default: all images; at most the session's img_vocab)."""
+    max_rows: most rows of one forward or backward call (default: all images; all averages the session can hand over, ready_cap)."""
 
     def __init__(self, session: GearSession, raw: torch.Tensor, Wd: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
                  adam: Optional["gb.gear_adam"] = None, max_norm: float = 1.0, max_rows: Optional[int] = None):
@@ -32,12 +32,13 @@ class NormedDensePart:
         D = session.p.dfv_dim
         if V != session.p.img_vocab or Wd.shape != (R, D) or (weight is not None and weight.shape != (R,)):
             raise ValueError("raw: [img_vocab][raw_dim], Wd: [raw_dim][dfv_dim], weight: [raw_dim]")
-        n = V if max_rows is None else int(max_rows)
-        if not 1 <= n <= V:
-            raise ValueError("max_rows in [1, img_vocab]")
+        n, back = (V, session.ready_cap) if max_rows is None else (int(max_rows), int(max_rows))
+        if not 1 <= n <= max(V, session.ready_cap):
+            raise ValueError("max_rows in [1, the larger of img_vocab and ready_cap]")
         dev = raw.device
         f = lambda *shape: torch.empty(shape, dtype=torch.float32, device=dev)
         self.session, self.raw, self.Wd, self.eps, self.max_rows, self.max_norm = session, raw, Wd, eps, n, max_norm
+        self.max_averages = back
         self.weight = torch.ones(R, dtype=torch.float32, device=dev) if weight is None else weight
         self.adam, self.t = adam or gb.make_adam(), 0
         blocks = lambda k: (k + gb.GEAR_Q8_BLOCK - 1) // gb.GEAR_Q8_BLOCK
@@ -46,9 +47,9 @@ class NormedDensePart:
         self.q, self.q_scale = e4m3_rows(n, R, dev), f(n, blocks(R))
         self.status = torch.zeros(2, dtype=torch.int32, device=dev)
         # the way back
-        self.h, self.dh = f(n, R), f(n, R)                       # normed rows; their gradient
-        self.g, self.g_scale = e4m3_rows(n, D, dev), f(n, blocks(D))
-        self.iota = torch.arange(n, dtype=torch.int32, device=dev)
+        self.h, self.dh = f(min(back, V), R), f(back, R)         # normed rows; their gradient
+        self.g, self.g_scale = e4m3_rows(back, D, dev), f(back, blocks(D))
+        self.iota = torch.arange(min(back, V), dtype=torch.int32, device=dev)
         self.Wd_grad, self.weight_grad = torch.zeros_like(Wd), torch.zeros_like(self.weight)
         self.norm_workspace = f(gb.GEAR_NORM_WORKSPACE_ROWS, R)
         self.clip_workspace = torch.empty(gb.GEAR_CLIP_WORKSPACE_BYTES, dtype=torch.uint8, device=dev)
@@ -72,13 +73,17 @@ class NormedDensePart:
     def backward(self, n: int, d_n=None):
         """Wd_grad and weight_grad from the averages the session handed over last (ready_ids, ready_avg).  The 8-bit rounding counts as
         none, except that the gradient goes back through the weights as they were used."""
-        if n > self.max_rows:
-            raise ValueError("more rows than max_rows")
+        if n > self.max_averages:
+            raise ValueError("more averages than max_rows, or than the session hands over")
         s = self.session
         ids = s.ready_ids
-        gb.gear_rms_norm(self.raw, self.weight, self.h, None, self.eps, ids=ids, n=n, d_n=d_n, status=self.status)
         self.Wd_grad.zero_()
-        gb.gear_dense_backward(s.ctx, self.h, self.iota, s.ready_avg, n, self.Wd_grad, d_n=d_n)
+        if n <= self.raw.shape[0]:                   # the images' normed rows, one for each average
+            gb.gear_rms_norm(self.raw, self.weight, self.h, None, self.eps, ids=ids, n=n, d_n=d_n, status=self.status)
+            gb.gear_dense_backward(s.ctx, self.h, self.iota, s.ready_avg, n, self.Wd_grad, d_n=d_n)
+        else:                                        # more averages than images (M completed groups are an average each): every image's once
+            gb.gear_rms_norm(self.raw, self.weight, self.h, None, self.eps, status=self.status)
+            gb.gear_dense_backward(s.ctx, self.h, ids, s.ready_avg, n, self.Wd_grad, d_n=d_n)
         gb.gear_q8_rows(s.ready_avg, self.g, self.g_scale, n=n, d_n=d_n)
         gb.gear_q8_matmul(self.g, self.g_scale, self.W8_t, self.W8_t_scale, self.dh, self.status, n=n, d_n=d_n)
         raw_grad = self.dh if self.raw.dtype == torch.float32 else self.dh.to(self.raw.dtype)

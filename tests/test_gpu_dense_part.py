@@ -127,6 +127,40 @@ def test_gradient_against_differences():
         s.close()
 
 
+def test_more_averages_than_images():
+    """A step may complete several groups of one image: its averages are bounded by its occurrences, not by the table."""
+    from paper_1806_03925_b200 import binding as gb
+    from paper_1806_03925_b200 import build, workloads
+    from paper_1806_03925_b200.dense_part import NormedDensePart
+    from paper_1806_03925_b200.session import DeviceBatch, GearSession
+    build.build()
+    p = workloads.PRESETS["tiny"].scaled(user_vocab=500, url_vocab=400, img_vocab=30, M=1, expire=5)
+    s = GearSession(p, workloads.head_params(p, 0), max_batch=256, max_nnz=1024, seed=0)
+    raw, R, D = torch.randn((p.img_vocab, 200), device="cuda"), 200, p.dfv_dim
+    part = NormedDensePart(s, raw, torch.randn((R, D), device="cuda") / 14)
+    b = DeviceBatch.from_host(workloads.BatchSource(p, 0).batch(0))
+    try:
+        s.forward_backward(b)
+        s.accumulate_collect_from_step(b, sync=False)
+        e = int(s.d_counts[0])
+        assert p.img_vocab < e <= b.nnz
+        part.backward(b.nnz, d_n=s.d_counts[0:1])
+        x, avg = raw[s.ready_ids[:e].long()].double(), s.ready_avg[:e].double()
+        xr = x * rms(x, part.eps)
+        h = xr * part.weight.double()
+        assert ((part.Wd_grad.double() - h.t() @ avg).abs() <= h.abs().t() @ avg.abs() * (rms_rel(R) + (e + 8) * U32) + 1e-30).all()
+        used = part.dh[:e].double()
+        assert ((part.weight_grad.double() - (used * xr).sum(0)).abs() <= (used * xr).abs().sum(0) * (rms_rel(R) + (e + 110) * U32) + 1e-30).all()
+        part.check()
+        with pytest.raises(ValueError):
+            part.backward(s.ready_cap + 1)
+        with pytest.raises(ValueError):
+            NormedDensePart(s, raw, part.Wd, max_rows=max(s.ready_cap, p.img_vocab) + 1)
+        assert NormedDensePart(s, raw, part.Wd, max_rows=s.ready_cap).max_rows == s.ready_cap
+    finally:
+        s.close()
+
+
 def test_bad_ids_and_refusals():
     gb, p, s, part, batches = make(max_rows=50)
     from paper_1806_03925_b200.dense_part import NormedDensePart
