@@ -5,7 +5,8 @@
 The way of a training program around GearSession: the images an expiry scan lists go through forward (events 2 and 3: their rows are
 normed, put into e4m3 and multiplied with the weights' 8-bit copy) to refresh_dfv; the averages a step hands over go through
 backward (event 6); step clips the gradients by their global norm, takes an Adam step and makes the 8-bit copies anew.
-No arithmetic happens here: every step is a call of the binding.
+No arithmetic happens here: every step is a call of the binding, but for one conversion: the norm's gradients take x and dout of one type, so
+where raw is bf16 the gradient of the normed rows is rounded to bf16 (2^-8 of each value at most) on its way to weight's.
 """
 from __future__ import annotations
 
@@ -72,7 +73,7 @@ class NormedDensePart:
 
     def backward(self, n: int, d_n=None):
         """Wd_grad and weight_grad from the averages the session handed over last (ready_ids, ready_avg).  The 8-bit rounding counts as
-        none, except that the gradient goes back through the weights as they were used."""
+        none, except that the gradient goes back through the weights as they were used; with bf16 raw rows it is rounded to bf16 behind them."""
         if n > self.max_averages:
             raise ValueError("more averages than max_rows, or than the session hands over")
         s = self.session
@@ -86,7 +87,7 @@ class NormedDensePart:
             gb.gear_dense_backward(s.ctx, self.h, ids, s.ready_avg, n, self.Wd_grad, d_n=d_n)
         gb.gear_q8_rows(s.ready_avg, self.g, self.g_scale, n=n, d_n=d_n)
         gb.gear_q8_matmul(self.g, self.g_scale, self.W8_t, self.W8_t_scale, self.dh, self.status, n=n, d_n=d_n)
-        raw_grad = self.dh if self.raw.dtype == torch.float32 else self.dh.to(self.raw.dtype)
+        raw_grad = self.dh if self.raw.dtype == torch.float32 else self.dh[:n].to(self.raw.dtype)
         gb.gear_rms_norm_backward(self.raw, self.weight, raw_grad, None, self.weight_grad, self.norm_workspace, self.eps, ids=ids, n=n, d_n=d_n,
                                   status=self.status)
 

@@ -127,6 +127,29 @@ def test_gradient_against_differences():
         s.close()
 
 
+def test_backward_of_few_averages_touches_few_rows():
+    """bf16 raw rows: what backward takes from the allocator, and converts, goes by its n."""
+    gb, p, s, part, batches = make(torch.bfloat16, 2000)
+    try:
+        s.forward_backward(batches[0])
+        s.accumulate_collect_from_step(batches[0], sync=False)
+        n = 16
+        part.backward(n, d_n=s.d_counts[0:1])
+        torch.cuda.synchronize()
+        torch.cuda.reset_peak_memory_stats()
+        held = torch.cuda.memory_allocated()
+        part.backward(n, d_n=s.d_counts[0:1])
+        torch.cuda.synchronize()
+        assert torch.cuda.max_memory_allocated() - held <= n * 2000 * 2 + 512
+        e = min(n, int(s.d_counts[0]))
+        x = part.raw[s.ready_ids[:e].long()].double()
+        xr, used = x * rms(x, part.eps), part.dh[:e].to(torch.bfloat16).double()
+        assert e > 0 and ((part.weight_grad.double() - (used * xr).sum(0)).abs() <= (used * xr).abs().sum(0) * (rms_rel(2000) + (e + 110) * U32) + 1e-30).all()
+        part.check()
+    finally:
+        s.close()
+
+
 def test_more_averages_than_images():
     """A step may complete several groups of one image: its averages are bounded by its occurrences, not by the table."""
     from paper_1806_03925_b200 import binding as gb
