@@ -20,7 +20,7 @@ LIB_PATH = os.path.join(_PKG, "libgear.so")
 GEAR_OK, GEAR_ERR_ARG, GEAR_ERR_CAPACITY, GEAR_ERR_BAD_ID, GEAR_ERR_CUDA, GEAR_ERR_STATE = 0, -1, -2, -3, -4, -5
 GEAR_F32, GEAR_BF16, GEAR_E4M3 = 0, 1, 2
 GEAR_ACC_SORT, GEAR_ACC_ATOMIC = 0, 1
-GEAR_DEV_BAD_ID, GEAR_DEV_READY_OVERFLOW, GEAR_DEV_OUT_CAPACITY, GEAR_DEV_BAD_CSR = 1, 2, 4, 8
+GEAR_DEV_BAD_ID, GEAR_DEV_READY_OVERFLOW, GEAR_DEV_OUT_CAPACITY, GEAR_DEV_BAD_CSR, GEAR_DEV_TIMEOUT = 1, 2, 4, 8, 16
 GEAR_TAG_USER, GEAR_TAG_URL, GEAR_TAG_DFV, GEAR_TAG_TS, GEAR_TAG_GRAD = 1, 2, 3, 4, 5
 GEAR_TABLE_USER, GEAR_TABLE_URL, GEAR_TABLE_DFV = 0, 1, 2
 

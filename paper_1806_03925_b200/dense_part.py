@@ -25,6 +25,8 @@ def e4m3_rows(n: int, cols: int, device="cuda") -> torch.Tensor:
 
 class NormedDensePart:
     """raw: [img_vocab][raw_dim] fp32 or bf16; Wd: [raw_dim][dfv_dim] fp32 and weight: [raw_dim] fp32, both updated in place by step.
+    forward and backward share no buffer that either writes and have a status each, so they may run on two streams; step (and requantise) writes what
+    both read, and belongs behind them and ahead of the next ones.  Calls of one way belong to one stream, or are ordered by the caller.
     max_rows: most rows of one forward or backward call (default: all images; all averages the session can hand over, ready_cap)."""
 
     def __init__(self, session: GearSession, raw: torch.Tensor, Wd: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
@@ -46,7 +48,9 @@ class NormedDensePart:
         self.W8, self.W8_scale = e4m3_rows(D, R, dev), f(blocks(D), blocks(R))
         self.W8_t, self.W8_t_scale = e4m3_rows(R, D, dev), f(blocks(R), blocks(D))
         self.q, self.q_scale = e4m3_rows(n, R, dev), f(n, blocks(R))
-        self.status = torch.zeros(2, dtype=torch.int32, device=dev)
+        # a status for each way, in one place
+        self._statuses = torch.zeros((2, 2), dtype=torch.int32, device=dev)
+        self.status, self.status_back = self._statuses[0], self._statuses[1]
         # the way back
         self.h, self.dh = f(min(back, V), R), f(back, R)         # normed rows; their gradient
         self.g, self.g_scale = e4m3_rows(back, D, dev), f(back, blocks(D))
@@ -80,16 +84,16 @@ class NormedDensePart:
         ids = s.ready_ids
         self.Wd_grad.zero_()
         if n <= self.raw.shape[0]:                   # the images' normed rows, one for each average
-            gb.gear_rms_norm(self.raw, self.weight, self.h, None, self.eps, ids=ids, n=n, d_n=d_n, status=self.status)
+            gb.gear_rms_norm(self.raw, self.weight, self.h, None, self.eps, ids=ids, n=n, d_n=d_n, status=self.status_back)
             gb.gear_dense_backward(s.ctx, self.h, self.iota, s.ready_avg, n, self.Wd_grad, d_n=d_n)
         else:                                        # more averages than images (M completed groups are an average each): every image's once
-            gb.gear_rms_norm(self.raw, self.weight, self.h, None, self.eps, status=self.status)
+            gb.gear_rms_norm(self.raw, self.weight, self.h, None, self.eps, status=self.status_back)
             gb.gear_dense_backward(s.ctx, self.h, ids, s.ready_avg, n, self.Wd_grad, d_n=d_n)
         gb.gear_q8_rows(s.ready_avg, self.g, self.g_scale, n=n, d_n=d_n)
-        gb.gear_q8_matmul(self.g, self.g_scale, self.W8_t, self.W8_t_scale, self.dh, self.status, n=n, d_n=d_n)
+        gb.gear_q8_matmul(self.g, self.g_scale, self.W8_t, self.W8_t_scale, self.dh, self.status_back, n=n, d_n=d_n)
         raw_grad = self.dh if self.raw.dtype == torch.float32 else self.dh[:n].to(self.raw.dtype)
         gb.gear_rms_norm_backward(self.raw, self.weight, raw_grad, None, self.weight_grad, self.norm_workspace, self.eps, ids=ids, n=n, d_n=d_n,
-                                  status=self.status)
+                                  status=self.status_back)
 
     def step(self, more: Sequence[torch.Tensor] = ()):
         """Clips the gradients of Wd and weight, and those in `more` (the head's), by their norm together; an Adam step on Wd and weight;
@@ -102,8 +106,9 @@ class NormedDensePart:
         self.requantise()
 
     def check(self):
-        """Raises if an ID was outside the table or a wait gave up since the last check; synchronises."""
-        bits, code = self.status.tolist()
-        if bits or code:
-            self.status.zero_()
-            raise gb.GearError(gb.GEAR_ERR_CUDA if bits & 16 else gb.GEAR_ERR_BAD_ID, "NormedDensePart", "status bits %d, code %d" % (bits, code))
+        """Raises if an ID was outside the table or a wait gave up since the last check; synchronises the current stream."""
+        (bits, code), (back_bits, back_code) = self._statuses.tolist()
+        if bits or code or back_bits or back_code:
+            self._statuses.zero_()
+            raise gb.GearError(gb.GEAR_ERR_CUDA if (bits | back_bits) & gb.GEAR_DEV_TIMEOUT else gb.GEAR_ERR_BAD_ID, "NormedDensePart",
+                               "forward: status bits %d, code %d; backward: %d, %d" % (bits, code, back_bits, back_code))

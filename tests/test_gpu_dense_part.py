@@ -150,6 +150,33 @@ def test_backward_of_few_averages_touches_few_rows():
         s.close()
 
 
+def test_a_wait_that_gave_up_on_one_way_leaves_the_other():
+    """Serving and training may run beside each other: what voids forward's results does not void backward's, and check tells."""
+    gb, p, s, part, batches = make(torch.float32, 2000)
+    try:
+        s.forward_backward(batches[0])
+        s.accumulate_collect_from_step(batches[0], sync=False)
+        part.backward(batches[0].nnz, d_n=s.d_counts[0:1])
+        e, want = int(s.d_counts[0]), part.weight_grad.clone()
+        part.check()
+        part.status[1] = 3
+        part.dh.fill_(7.0)
+        part.backward(batches[0].nnz, d_n=s.d_counts[0:1])
+        assert torch.equal(part.weight_grad, want) and not (part.dh[:e] == 7.0).all(1).any()
+        rows = torch.full((p.img_vocab, p.dfv_dim), 7.0, device="cuda")
+        part.forward(torch.arange(p.img_vocab, dtype=torch.int32, device="cuda"), rows)
+        assert (rows == 7.0).all()
+        with pytest.raises(gb.GearError) as err:
+            part.check()
+        assert err.value.code == gb.GEAR_ERR_CUDA
+        part.check()
+        part.forward(torch.arange(p.img_vocab, dtype=torch.int32, device="cuda"), rows)
+        assert not (rows == 7.0).any()
+        part.check()
+    finally:
+        s.close()
+
+
 def test_more_averages_than_images():
     """A step may complete several groups of one image: its averages are bounded by its occurrences, not by the table."""
     from paper_1806_03925_b200 import binding as gb
