@@ -948,7 +948,7 @@ static int check_norm(const NormArgs& a, int32_t dtype) {
     if (a.n < 0 || a.n > INT32_MAX) return arg_fail("n outside [0, 2^31 - 1]");
     if (a.cols < 1 || a.cols > MAX_COLS) return arg_fail("cols outside [1, 2^31 - 1024]");
     if (!(a.eps >= 0.f)) return arg_fail("eps >= 0");
-    if (a.ids && (a.vocab < 1 || a.vocab > INT32_MAX)) return arg_fail("vocab outside [1, 2^31 - 1]");
+    if (a.ids && (a.vocab < (a.n > 0) || a.vocab > INT32_MAX)) return arg_fail("vocab outside [1, 2^31 - 1] (0 where there are no rows)");
     if (a.n > 0 && (!a.x || a.ldx < a.cols || !aligned_to(a.x, dtype))) return arg_fail("x: NULL, misaligned or ldx < cols");
     if (a.weight && !aligned_to(a.weight, GEAR_F32)) return arg_fail("weight: misaligned");
     return GEAR_OK;

@@ -64,6 +64,14 @@ def test_rows_too_long_to_step_over_are_refused(gb):
             assert b"bad argument" in L.gear_last_error()
 
 
+def test_no_rows_by_id_of_an_empty_table(gb):
+    """Nothing to do: as with no rows of any other table.  (A row needs a table.)"""
+    L = gb.load()
+    assert L.gear_rms_norm(*dict(NORM, x=None, ids=P, vocab=0, n=0).values()) == gb.GEAR_OK
+    assert L.gear_rms_norm_backward(*dict(BACK, x=None, ids=P, vocab=0, n=0, dweight=None, workspace=None).values()) == gb.GEAR_OK
+    assert L.gear_rms_norm(*dict(NORM, ids=P, vocab=0, n=1).values()) == L.gear_rms_norm(*dict(NORM, ids=P, vocab=-1, n=0).values()) == gb.GEAR_ERR_ARG
+
+
 def test_misaligned_scales_of_weights_are_refused(gb):
     for wrong in (dict(scale=P + 2), dict(scale_t=P + 1), dict(q=None, scale_t=P + 2), dict(q_t=None, scale=P + 3)):
         assert gb.load().gear_q8_weights(*dict(WEIGHTS, **wrong).values()) == gb.GEAR_ERR_ARG, wrong
