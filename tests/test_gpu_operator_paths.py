@@ -167,3 +167,30 @@ def test_gradients_of_very_small_rows(gb, n, cols, dtype):
         assert ((dx.double() - want).abs() <= allowed).all()
         size = (g.double() * xd).abs() * r
         assert ((dw.double() - dw64).abs() <= (size * (rms_rel(cols) + (n / 592 + 110) * U32 + 0.6 * small)).sum(0) + 1e-44).all()
+
+
+# ------------------------------------------------------------------------------------------------ the 8-bit quotient
+def to_e4m3(x):
+    """64-bit values of at most 448 rounded once to e4m3 (nearest, ties to even): steps of 2^(exponent - 3), 2^-9 below 2^-6."""
+    step = torch.exp2(torch.floor(torch.log2(x.abs().clamp_min(2.0 ** -6))) - 3)
+    return (torch.round(x / step) * step).clamp(-448, 448)
+
+
+@pytest.mark.parametrize("dtype,cols", [(F32, 1536), (F32, 1001), (BF16, 1536)])
+def test_quotients_are_rounded_as_divisions_are(gb, dtype, cols):
+    """The quotient v / (largest / 448) is rounded to fp32 once, half a step or 2^-24 of it, and then to e4m3: a value differs from the quotient
+    rounded to e4m3 at once only where the quotient lies that near to the middle between two e4m3 values.  What the quotient's correction itself
+    leaves: its remainder, 2^-22 of the value, comes with roundings of 2^-24 and a reciprocal off by 2^-23, so 2^-44; the factor 1 + 2^-8 is more."""
+    off = 0
+    for seed in range(8):
+        n = 1000
+        x = (randn((n, cols), seed) * torch.logspace(-12, 12, n, device="cuda")[:, None]).to(dtype)
+        q, s = e4m3_rows(n, cols), torch.empty((n, blocks(cols)), device="cuda")
+        gb.gear_q8_rows(x, q, s)
+        exact = x.double() * 448 / spread(block_amax(x.double()), cols)
+        want, got = to_e4m3(exact), q.double()
+        differs = want != got
+        middle = (want + got) / 2
+        assert ((exact - middle).abs()[differs] <= exact.abs()[differs] * U32 * (1 + 2.0 ** -8)).all()
+        off += int(differs.sum())
+    assert off < 1e-4 * 8 * 1000 * cols           # (the share of values so near to a middle: 2^-24 against a spacing of 2^-3 to 2^-4)
