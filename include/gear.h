@@ -468,7 +468,8 @@ int gear_q8_matmul(const void* a, int64_t lda, const float* a_scale, const void*
  * grads: host array of `count` tensors; grad: device, n values of dtype GEAR_F32 or GEAR_BF16, any alignment of a value's own size; out: the tensor's grad
  * itself (which is left untouched where c = 1) or memory that overlaps no tensor of the call; not read by gear_grad_norm.
  * A tensor may be empty, the list too (norm 0, c = 1).  norm: device fp32 [2].  A norm that is not finite is not hidden: an infinity among the
- * gradients gives c = 0 and a NaN in its place, a NaN gives NaN everywhere.  workspace: device, GEAR_CLIP_WORKSPACE_BYTES, 8-byte aligned,
+ * gradients gives c = 0 and a NaN in its place, a NaN gives NaN everywhere.  An infinite max_norm clips nothing (c = 1) as long as the norm is finite;
+ * an infinite norm then gives NaN everywhere.  workspace: device, GEAR_CLIP_WORKSPACE_BYTES, 8-byte aligned,
  * one for every stream; nothing in it carries over from one call to the next.  Results do not depend on timing.
  */
 enum { GEAR_CLIP_WORKSPACE_BYTES = 32768 };

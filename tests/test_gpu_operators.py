@@ -578,6 +578,17 @@ def test_clip_extremes(gb):
     assert norm.isnan().all() and g.isnan().all()
 
 
+def test_clip_to_an_infinite_norm(gb):
+    ws, norm = workspace(gb), torch.empty(2, device="cuda")
+    g = [randn((5000,), 1) * 1e30, randn((333,), 2).to(BF16)]
+    outs = [torch.empty_like(t) for t in g]
+    gb.gear_clip_grads(g, float("inf"), norm, ws, outs=outs)
+    assert norm[0].isfinite() and float(norm[1]) == 1.0 and all(torch.equal(a, b) for a, b in zip(g, outs))
+    g[0][7] = float("inf")
+    gb.gear_clip_grads(g, float("inf"), norm, ws, outs=outs)
+    assert float(norm[0]) == float("inf") and norm[1].isnan() and outs[0].isnan().all() and outs[1].isnan().all()
+
+
 def test_clip_beyond_32_bits(gb):
     n = (1 << 31) + 77
     g = torch.full((n,), 0.5, dtype=BF16, device="cuda")
