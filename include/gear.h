@@ -430,7 +430,8 @@ int gear_rms_norm(const void* x, int64_t ldx, int32_t dtype, const int32_t* ids,
  *     dx[k] = r g - x r^3 (sum_j g_j x_j) / cols (+ dres[k]);      dweight_j = sum_k dout[k]_j x[k]_j r[k]   (written, not added to)
  * x, dout, dres (optional: the gradient that reaches y past the norm), dx: dtype.  ids / vocab as above (for x alone; then dx and dres belong to row k).
  * dx or dweight may be NULL; dx may be dout or dres.  8-bit outputs count as unrounded.  workspace: fp32
- * [GEAR_NORM_WORKSPACE_ROWS][cols], 16-byte aligned, when dweight is given.  Results do not depend on timing.
+ * [GEAR_NORM_WORKSPACE_ROWS][cols], 16-byte aligned, when dweight is given; one for every stream,
+ * nothing in it carries over from one call to the next.  Results do not depend on timing.
  */
 enum { GEAR_NORM_WORKSPACE_ROWS = 592 };
 int gear_rms_norm_backward(const void* x, int64_t ldx, int32_t dtype, const int32_t* ids, int64_t vocab, const float* weight,

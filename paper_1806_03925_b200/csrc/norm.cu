@@ -721,7 +721,7 @@ q8_weights_kernel(const float* __restrict__ W, int64_t ldw, int vec, int K, int 
 // ---------------------------------------------------------------- host side
 static bool on16(const void* p, int64_t ld, int size) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && (ld * size) % 16 == 0; }
 
-// whether all rows start on 16-byte boundaries and hold whole vectors (an 8-bit row: on 8-byte boundaries, a lane's piece of it)
+// whether all rows, 8-bit ones too, start on 16-byte boundaries and hold whole vectors of the input's type
 static bool vectors(const NormArgs& a, int size) {
     const int64_t vec = 16 / size;
     if (a.cols % vec || !on16(a.x, a.ldx, size) || (a.weight && !on16(a.weight, 0, 4))) return false;

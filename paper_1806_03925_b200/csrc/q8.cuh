@@ -37,7 +37,7 @@ __device__ __forceinline__ float q8_larger(float a, float b, float c) {
 //     scale = max(r largest, 2^-100) / 448,   q = r v / scale.
 // r cancels out of the quotient, so q is v / (largest / 448), for which nothing has to be known of r yet: values go out before the
 // row's sum of squares is there.  The divisor is kept in two parts, and the quotient is rounded once, as a division is (the product with
-// the reciprocal, corrected by its remainder), so that a value lands on the other side of the middle between two e4m3 values only where
+// an approximate reciprocal, corrected by its remainder in a fused multiply-add: P. Markstein, IBM J. Res. Dev. 34, 1990), so that a value lands on the other side of the middle between two e4m3 values only where
 // that rounding, or those of v and of the block's largest, have put it there.  Where that does not hold (largest infinite, a NaN, below 2^-90, or r largest below 2^-100: q8_usual) the
 // block is written by the definition (Q8Plain).
 // (Blocks of zeros are usual too: zeros, and the smallest scale.)

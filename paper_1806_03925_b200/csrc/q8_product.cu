@@ -9,13 +9,14 @@
 // factor per block of K; two columns are multiplied and added per instruction (fma.rn.f32x2).
 //
 // Bound by the chain of a tile's two accumulators where tiles are 256 wide (products issued to accumulator complete 1050 cycles, read and
-// added 640, handed back 250: 970 per block of K with 512 of products in it): 131072 x 2048 x 1024 in 276 us, 1990 TFLOP/s; by memory
-// where the output is narrow (262144 x 1536 x 64 in fp32: 75 us, 0.98 of the copy rate).
+// added 640, handed back 250: 970 per block of K with 512 of products in it): 131072 x 2048 x 1024 in 274 us, 2000 TFLOP/s, in a graph
+// (in a run of calls, under the power cap, 321 us); by memory where the output is narrow (262144 x 1536 x 64 in fp32: 75 us, 0.98 of the copy rate).
 //
 // One persistent kernel, a CTA per SM: warps 0 and 3 stream the operands in by TMA (boxes of 128 bytes along K, which are one block),
 // warps 1 and 2 issue the products (M 128, N BN, K 32: four per block), warps 4 to 11 add up and store.  Two warps share a quarter of the
 // tensor-memory lanes and split the columns.  Every wait is bounded: on a timeout the kernel says so in the status words, leaves
-// its loops, frees its tensor memory and returns.  No cluster launch and no multicast.
+// its loops, waits (bounded again) for the copies and products under way, frees its tensor memory and returns.  No cluster
+// launch and no multicast.
 #include <type_traits>
 
 #include "internal.h"

@@ -97,7 +97,8 @@ class NormedDensePart:
 
     def step(self, more: Sequence[torch.Tensor] = ()):
         """Clips the gradients of Wd and weight, and those in `more` (the head's), by their norm together; an Adam step on Wd and weight;
-        their 8-bit copies.  norm holds the norm and the factor."""
+        their 8-bit copies.  norm holds the norm and the factor.  (t counts on the host: a step that is captured and replayed repeats one t.  With `more`
+        the list of gradients is made anew each time.)"""
         grads = self.grads if not more else [self.Wd_grad, self.weight_grad, *more]
         gb.gear_clip_grads(grads, self.max_norm, self.norm, self.clip_workspace)
         self.t += 1
