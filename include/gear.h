@@ -418,7 +418,8 @@ enum { GEAR_Q8_BLOCK = 128 };
  * x, res, res_out: dtype GEAR_F32 or GEAR_BF16.  ids (device, optional): rows of x by ID in [0, vocab); an ID outside counts as a row of zeros and
  * raises GEAR_DEV_BAD_ID.  res, res_out: optional, each without the other too; res_out may be res, or x where ids is NULL.
  * weight: fp32 [cols], optional (ones).  out_dtype GEAR_F32, GEAR_BF16 (scale NULL) or GEAR_E4M3 with scale fp32 [n][ceil(cols / 128)].
- * Sums are fp32; with a GEAR_E4M3 output h is not rounded to any other type in between.
+ * Sums are fp32 (squares and sums outside its range become infinities or zeros as fp32 has it); with a GEAR_E4M3 output h is not rounded to any other
+ * type in between.
  */
 int gear_rms_norm(const void* x, int64_t ldx, int32_t dtype, const int32_t* ids, int64_t vocab, const void* res, int64_t ld_res,
                   void* res_out, int64_t ld_res_out, const float* weight, int64_t n, const int64_t* d_n, int32_t cols, float eps,

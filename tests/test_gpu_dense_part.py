@@ -177,6 +177,38 @@ def test_a_wait_that_gave_up_on_one_way_leaves_the_other():
         s.close()
 
 
+@pytest.mark.parametrize("raw_dtype", [torch.float32, torch.bfloat16])
+def test_both_ways_beside_each_other(raw_dtype):
+    """forward on one stream, backward on another, over and over: what either gives alone."""
+    gb, p, s, part, batches = make(raw_dtype, 1000)
+    try:
+        s.forward_backward(batches[0])
+        s.accumulate_collect_from_step(batches[0], sync=False)
+        ids = torch.arange(p.img_vocab, dtype=torch.int32, device="cuda")
+        want, rows = torch.empty((p.img_vocab, p.dfv_dim), device="cuda"), [torch.full((p.img_vocab, p.dfv_dim), 7.0, device="cuda") for _ in range(20)]
+        part.forward(ids, want)
+        part.backward(batches[0].nnz, d_n=s.d_counts[0:1])
+        e, grad = int(s.d_counts[0]), part.weight_grad.clone()
+        dh, Wd_grad = part.dh[:e].clone(), part.Wd_grad.clone()
+        one, two = torch.cuda.Stream(), torch.cuda.Stream()
+        torch.cuda.synchronize()
+        grads = []
+        for r in rows:
+            with torch.cuda.stream(one):
+                part.forward(ids, r)
+            with torch.cuda.stream(two):
+                part.backward(batches[0].nnz, d_n=s.d_counts[0:1])
+                grads.append((part.weight_grad.clone(), part.dh[:e].clone()))
+        torch.cuda.synchronize()
+        part.check()
+        assert all(torch.equal(r, want) for r in rows)
+        assert all(torch.equal(a, grad) and torch.equal(b, dh) for a, b in grads)
+        # (its sums are in an order the hardware picks)
+        assert ((part.Wd_grad - Wd_grad).abs() <= part.h[:e].abs().t() @ s.ready_avg[:e].abs() * (2 * (e + 8) * U32) + 1e-30).all()
+    finally:
+        s.close()
+
+
 def test_more_averages_than_images():
     """A step may complete several groups of one image: its averages are bounded by its occurrences, not by the table."""
     from paper_1806_03925_b200 import binding as gb
