@@ -399,7 +399,7 @@ int gear_adam_dense(float* param, const float* grad, float* m, float* v, int64_t
  *   - d_n (device, optional): only rows k < min(n, *d_n) are computed, *d_n read when the kernel runs; the others stay as they were;
  *   - status (device, two words, zero before the first call; optional unless said otherwise): GEAR_DEV_* bits are added to
  *     status[0]; status[1] is non-zero once a bounded wait has given up (GEAR_DEV_TIMEOUT), and until the caller clears it: until
- *     then products raise GEAR_DEV_TIMEOUT again and may leave their outputs as they were.
+ *     then a product may raise GEAR_DEV_TIMEOUT again and leave its output as it was.
  *     Calls on streams that may overlap each have a status of their own;
  *   - inputs and outputs do not overlap, except where said; all pointers belong to the current device;
  *   - a stream under capture takes them like any other, after a first call of the same kind outside of a capture.
